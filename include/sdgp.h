@@ -69,7 +69,8 @@ typedef enum { SDGP_RANDOM = 0, SDGP_MAGNITUDE = 1, SDGP_RESCALED_MAGNITUDE = 2 
 /* Element type of the 16-bit tensors of the *_typed entry points (the un-suffixed ones are bf16). */
 typedef enum {
   SDGP_BF16 = 0, /* bfloat16 */
-  SDGP_FP16 = 1  /* IEEE binary16, the precision the paper's experiments trained in (Section 4) */
+  SDGP_FP16 = 1, /* IEEE binary16, the precision the paper's experiments trained in (Section 4) */
+  SDGP_FP32 = 2  /* IEEE binary32: only where an entry point says so, SDGP_ERR_INVALID_ARG elsewhere */
 } sdgp_dtype;
 
 /* `flags` of the dgrad entry points. */
@@ -209,6 +210,38 @@ sdgp_status sdgp_residual_relu_backward_prune(const void* dY, const void* dSkip,
 sdgp_status sdgp_maxpool_relu_backward_prune(const void* dYp, const void* dSkipP, const void* act, int B, int H, int Wd, int64_t K, int n, int m,
                                              sdgp_scheme scheme, uint64_t seed, sdgp_dtype dtype, void* grad, void* dOp_dense,
                                              void* values, void* meta, void* mask, void* stream);
+
+/* ---- Operators around the linear layers of a language model. They have no counterpart in the paper's networks; what joins them to
+ * its method is that the gradient passes hand the pruned dL/dO (Algorithm 1) to the layer below, as the producers above do. Element
+ * type `dtype` (SDGP_BF16, SDGP_FP16 or SDGP_FP32) of all tensors whose type is not given; statistics and sums in fp32. Vectors of
+ * fp32 or int64 need their own type's alignment only. ---- */
+
+/* Log probabilities of given tokens. logits [rows, K], of which the first `classes` columns are tokens (1 <= classes <= K; the others
+ * are padding of the layer that made them and are not read), targets [rows] int64. With lse = log sum_j exp(logits[r, j]):
+ *   logprob [rows] f32      logits[r, t] - lse; 0 for a negative target (a token that is not counted), NaN for a target >= classes
+ *   entropy [rows] f32      - sum_j p_j log p_j                                                                - optional
+ *   lse     [rows] f32      what the backward pass wants                                                       - optional
+ *   top_logprob [rows, top] f32, top_token [rows, top] int64: the `top` largest logits of the row in descending order, equal ones by
+ *                           the lower token first (0 <= top <= 32, top <= classes; a NaN is never one: where a row has fewer
+ *                           numbers than `top`, the rest are token -1, NaN)                                    - each optional
+ * A logit of -infinity has probability 0. A row of nothing but -infinity: lse and all log probabilities -infinity, entropy 0. A NaN or
+ * +infinity among the logits makes lse, entropy and log probabilities of its row NaN. Any K: rows need not start on a 16-byte boundary. */
+sdgp_status sdgp_token_logprob(const void* logits, const int64_t* targets, int64_t rows, int64_t K, int64_t classes, sdgp_dtype dtype,
+                               int top, float* logprob, float* entropy, float* lse, float* top_logprob, int64_t* top_token,
+                               void* stream);
+
+/* Its gradient, the dL/dO of the layer that made the logits, and Algorithm 1 on it in the same pass. From lse and entropy of
+ * sdgp_token_logprob and the gradients d_logprob [rows], d_entropy [rows] (f32, each may be null: zero; entropy is only read with
+ * d_entropy):
+ *   dL/dO[r, j] = d_logprob (1[j = t] - p_j) - d_entropy p_j (log p_j + entropy),  +0.0 for j >= classes,
+ * where a negative target takes no d_logprob and a target >= classes makes its row NaN; a row whose lse is -infinity gets zeros.
+ *   grad   [rows, K]                      - optional; may be `logits` itself
+ *   values [rows, K/2], meta [rows, K/16]: the compressed pruned copy, as sdgp_prune (16-bit types only, n <= 2, K % m == 0,
+ *                                           K % 16 == 0)  - each optional; n, m, scheme and seed are only looked at with them */
+sdgp_status sdgp_token_logprob_backward(const void* logits, const int64_t* targets, const float* lse, const float* entropy,
+                                        const float* d_logprob, const float* d_entropy, int64_t rows, int64_t K, int64_t classes, int n,
+                                        int m, sdgp_scheme scheme, uint64_t seed, sdgp_dtype dtype, void* grad, void* values, void* meta,
+                                        void* stream);
 
 /* Data gradient of a GROUPED convolution (the 3x3 convolutions of RegNetX, one of the networks of Section 4; the
  * contraction is Section 2.1 / Fig. 2 and Section 3.1 / Fig. 3 with the sum over output channels restricted to the

@@ -17,12 +17,13 @@ from . import build as _build
 RANDOM, MAGNITUDE, RESCALED_MAGNITUDE = 0, 1, 2
 FLAG_TWO_PASS, FLAG_FUSED, FLAG_DENSE, FLAG_MASKED, FLAG_CHANNEL = 0, 1, 2, 3, 4
 
-BF16, FP16 = 0, 1   # sdgp_dtype
+BF16, FP16, FP32 = 0, 1, 2   # sdgp_dtype (FP32: only the operators around a language model's linear layers)
 EXPORTS = ["sdgp_prune", "sdgp_dgrad_linear", "sdgp_dgrad_conv2d", "sdgp_spmm_linear", "sdgp_spmm_conv2d",
            "sdgp_prune_typed", "sdgp_dgrad_linear_typed", "sdgp_dgrad_conv2d_typed", "sdgp_spmm_linear_typed",
            "sdgp_spmm_conv2d_typed", "sdgp_channel_scales", "sdgp_relu_backward_prune", "sdgp_residual_relu_backward_prune", "sdgp_maxpool_relu_backward_prune", "sdgp_dgrad_linear_static", "sdgp_selftest_bounded_wait", "sdgp_selftest_plan",
            "sdgp_workspace_size_linear", "sdgp_workspace_size_conv2d", "sdgp_workspace_size_conv2d_grouped",
            "sdgp_dgrad_conv2d_grouped", "sdgp_last_device_error",
+           "sdgp_token_logprob", "sdgp_token_logprob_backward",
            "sdgp_status_string"]
 
 _lib = None
@@ -91,6 +92,10 @@ def lib() -> ctypes.CDLL:
         L.sdgp_selftest_bounded_wait.restype = i32
         L.sdgp_selftest_plan.argtypes = [i32] * 13 + [u32, ctypes.POINTER(i32)]
         L.sdgp_selftest_plan.restype = i32
+        L.sdgp_token_logprob.argtypes = [vp, vp, i64, i64, i64, i32, i32, vp, vp, vp, vp, vp, vp]
+        L.sdgp_token_logprob.restype = i32
+        L.sdgp_token_logprob_backward.argtypes = [vp] * 6 + [i64, i64, i64, i32, i32, i32, u64, i32, vp, vp, vp, vp]
+        L.sdgp_token_logprob_backward.restype = i32
         L.sdgp_status_string.argtypes = [i32]
         L.sdgp_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -245,6 +250,26 @@ def sdgp_channel_scales(dO, n, m, dtype, out):
     if out.numel() < 3 * K or out.element_size() != 4:
         raise ValueError("out must hold 3*K float32 values")
     _check(lib().sdgp_channel_scales(_ptr(dO), rows, K, n, m, dtype, _ptr(out), _stream()), "sdgp_channel_scales")
+
+
+# ---- operators around a language model's linear layers: the work goes to the current stream of the tensors' device, whichever
+# device is current; element types are checked against `dtype` ----
+
+
+def sdgp_token_logprob(logits, targets, logprob, entropy=None, lse=None, top_logprob=None, top_token=None, classes=None, dtype=BF16):
+    """``sdgp_token_logprob``: log probabilities of the tokens ``targets`` (int64) under ``logits``, whose last dimension is K and
+    holds ``classes`` tokens (default: all of it). ``logprob``, ``entropy`` and ``lse`` hold one float32 a row, ``top_logprob``
+    (float32) and ``top_token`` (int64) the same number of alternatives a row. Outputs are caller-allocated (or None)."""
+    _check((_torch or _load()).token_logprob(logits, targets, classes, dtype, logprob, entropy, lse, top_logprob, top_token),
+           "sdgp_token_logprob")
+
+
+def sdgp_token_logprob_backward(logits, targets, lse, d_logprob, grad=None, entropy=None, d_entropy=None, n=2, m=4, scheme=MAGNITUDE,
+                                seed=0, dtype=BF16, values=None, meta=None, classes=None):
+    """``sdgp_token_logprob_backward``: ``grad`` = dL/dO of the layer that made ``logits`` (it may be ``logits`` itself),
+    ``values`` and ``meta`` its compressed pruned copy, in one pass."""
+    _check((_torch or _load()).token_logprob_backward(logits, targets, lse, entropy, d_logprob, d_entropy, classes, n, m, scheme, seed,
+                                                      dtype, grad, values, meta), "sdgp_token_logprob_backward")
 
 
 def sdgp_selftest_bounded_wait():

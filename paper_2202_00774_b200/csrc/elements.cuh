@@ -1,0 +1,88 @@
+// Elements of the tensors of the language-model kernels (logprob.cu, norm.cu, fp8_quantize.cu): bf16, binary16 or fp32 in memory, fp32 in
+// registers, eight at a time.
+#pragma once
+#include "prune_core.cuh"
+
+namespace sdgp {
+namespace {
+
+template <int DT>
+struct Element {  // DT: sdgp_dtype
+  static constexpr bool kF16 = DT == SDGP_FP16;
+  static constexpr bool k32 = DT == SDGP_FP32;
+  static constexpr int kBytes = k32 ? 4 : 2;
+
+  static __device__ __forceinline__ float load(const void* p, int64_t i) {
+    if constexpr (k32) return ((const float*)p)[i];
+    else return lane_lo<kF16>((uint32_t)((const uint16_t*)p)[i]);
+  }
+  static __device__ __forceinline__ void store(void* p, int64_t i, float x) {
+    if constexpr (k32) ((float*)p)[i] = x;
+    else ((uint16_t*)p)[i] = (uint16_t)f32_to_elem_bits<kF16>(x);
+  }
+  // Eight elements as they lie in memory (16 bytes, or 32 of fp32); `i` a multiple of 8 and the tensor 16-byte aligned.
+  struct Raw {
+    uint4 a, b;  // b: fp32 only
+  };
+  static __device__ __forceinline__ Raw load8(const void* p, int64_t i) {
+    Raw r;
+    const uint4* q = (const uint4*)((const uint8_t*)p + i * kBytes);
+    r.a = q[0];
+    r.b = k32 ? q[1] : make_uint4(0u, 0u, 0u, 0u);
+    return r;
+  }
+  static __device__ __forceinline__ void widen(const Raw& r, float (&x)[8]) {
+    if constexpr (k32) {
+      const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
+    } else {
+      const uint32_t w[4] = {r.a.x, r.a.y, r.a.z, r.a.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[2 * e] = lane_lo<kF16>(w[e]);
+        x[2 * e + 1] = lane_hi<kF16>(w[e]);
+      }
+    }
+  }
+  // Rounded to nearest even.
+  static __device__ __forceinline__ Raw narrow(const float (&x)[8]) {
+    Raw r;
+    if constexpr (k32) {
+      r.a = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+      r.b = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+    } else {
+      r.a = make_uint4(pack_pair_rn<kF16>(x[0], x[1]), pack_pair_rn<kF16>(x[2], x[3]), pack_pair_rn<kF16>(x[4], x[5]),
+                       pack_pair_rn<kF16>(x[6], x[7]));
+      r.b = make_uint4(0u, 0u, 0u, 0u);
+    }
+    return r;
+  }
+  static __device__ __forceinline__ void store8(void* p, int64_t i, const Raw& r) {
+    uint4* q = (uint4*)((uint8_t*)p + i * kBytes);
+    q[0] = r.a;
+    if (k32) q[1] = r.b;
+  }
+};
+
+// The larger of two numbers; NaN if one of them is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+  return x;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {  // 2^x, relative error about 2^-22; subnormal results are zero
+  float d;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
+  return d;
+}
+
+}  // namespace
+}  // namespace sdgp

@@ -114,6 +114,14 @@ bool query_grouped(int B, int H, int W, int C, int groups, int R, int S, int str
 bool query_parities(bool sparse, int B, int H, int W, int Cin, int Cout, int R, int S, int stride, int pad, const StoredChannels* stored,
                     const ConvGroups* conv_groups, int* plan);
 
+// Log probabilities of tokens and their gradient (logprob.cu); null pointers and shapes as sdgp.h says, checked by the caller.
+cudaError_t launch_token_logprob(const void* logits, const int64_t* targets, int64_t rows, int64_t K, int64_t classes, int dtype, int top,
+                                 float* logprob, float* entropy, float* lse, float* top_logprob, int64_t* top_token, cudaStream_t stream);
+cudaError_t launch_token_logprob_backward(const void* logits, const int64_t* targets, const float* lse, const float* entropy,
+                                          const float* d_logprob, const float* d_entropy, int64_t rows, int64_t K, int64_t classes, int n,
+                                          int m, int scheme, uint64_t seed, int dtype, void* grad, void* values, void* meta,
+                                          cudaStream_t stream);
+
 // Launches a one-CTA kernel whose only wait can never be satisfied (50 ms limit).
 sdgp_status launch_bounded_wait_selftest(cudaStream_t stream);
 

@@ -6,10 +6,13 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <Python.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
+
+#include <algorithm>
 
 #include "../../include/sdgp.h"
 #include "torch_autograd.h"
@@ -267,6 +270,136 @@ ENTRY(spmm_conv2d) {  // values, meta, W, dD, stride, pad, dtype
   });
 }
 
+// ---- operators around a language model's linear layers ----
+
+// Reads arguments like Args; every tensor must lie on the device of the first one and have the element type that it stands for.
+struct LmArgs : Args {
+  using Args::Args;
+  c10::Device device{c10::kCUDA, 0};
+  bool any = false;
+
+  PyObject* fail(const char* name, const char* what) {
+    if (ok) PyErr_Format(PyExc_ValueError, "%s %s", name, what);
+    ok = false;
+    return nullptr;
+  }
+  const at::Tensor* on_device(const char* name) {
+    const at::Tensor* t = tensor(name);
+    if (!t) return nullptr;
+    if (any && t->device() != device) {
+      fail(name, "must be on the same device as the other tensors");
+      return nullptr;
+    }
+    device = t->device();
+    any = true;
+    return t;
+  }
+  // Elements of `dtype`: 16-bit (any type, as elsewhere in this library) or float32.
+  const at::Tensor* elements(const char* name, int dtype) {
+    const at::Tensor* t = on_device(name);
+    if (t && (dtype == SDGP_FP32 ? t->scalar_type() != at::kFloat : t->element_size() != 2)) {
+      fail(name, "does not have the elements that dtype names");
+      return nullptr;
+    }
+    return t;
+  }
+  const at::Tensor* of_type(const char* name, at::ScalarType type, int64_t numel) {
+    const at::Tensor* t = on_device(name);
+    if (t && t->scalar_type() != type) {
+      fail(name, type == at::kFloat ? "must be a float32 tensor" : "must be an int64 tensor");
+      return nullptr;
+    }
+    if (t && numel >= 0 && t->numel() != numel) {
+      fail(name, "does not have the number of elements that the other shapes ask for");
+      return nullptr;
+    }
+    return t;
+  }
+  void same_numel(const char* name, const at::Tensor* t, int64_t numel) {
+    if (t && t->numel() != numel) fail(name, "does not have the number of elements that the other shapes ask for");
+  }
+};
+
+void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+float* floats(const at::Tensor* t) { return (float*)data(t); }
+
+template <class F>
+PyObject* status_on(const LmArgs& in, F call) {
+  if (!in.ok) return nullptr;
+  const c10::cuda::CUDAGuard guard(in.device);
+  return status_of(in, call);
+}
+
+// An integer, or `otherwise` for None.
+int64_t i64_or(Args& in, int64_t otherwise) {
+  if (in.ok && *in.a == Py_None) {
+    ++in.a;
+    return otherwise;
+  }
+  return in.i64();
+}
+
+// A tensor argument that must be there.
+const at::Tensor* given(LmArgs& in, const at::Tensor* t, const char* name) {
+  if (in.ok && !t) in.fail(name, "must be a tensor, not None");
+  return t;
+}
+
+ENTRY(token_logprob) {  // logits, targets, classes, dtype, logprob, entropy, lse, top_logprob, top_token
+  LmArgs in(args, nargs, 9);
+  const int dtype = nargs == 9 ? (int)PyLong_AsLong(args[3]) : 0;
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* logits = given(in, in.elements("logits", dtype), "logits");
+  int64_t rows = 0, K = 0;
+  if (in.ok) rows_and_k(logits, rows, K);
+  const at::Tensor* targets = given(in, in.of_type("targets", at::kLong, rows), "targets");
+  const int64_t classes = i64_or(in, K);
+  in.i32();
+  const at::Tensor* logprob = given(in, in.of_type("logprob", at::kFloat, rows), "logprob");
+  const at::Tensor *entropy = in.of_type("entropy", at::kFloat, rows), *lse = in.of_type("lse", at::kFloat, rows),
+                   *top_logprob = in.of_type("top_logprob", at::kFloat, -1), *top_token = in.of_type("top_token", at::kLong, -1);
+  int64_t top = 0;
+  for (const at::Tensor* t : {top_logprob, top_token}) {
+    if (!in.ok || !t) continue;
+    const int64_t k = t->dim() ? t->size(-1) : 0;
+    in.same_numel("top_logprob or top_token", t, rows * k);
+    if (in.ok && top != 0 && k != top) in.fail("top_logprob and top_token", "must have the same shape");
+    top = k;
+  }
+  return status_on(in, [&](void* s) {
+    return sdgp_token_logprob(data(logits), (const int64_t*)data(targets), rows, K, classes, (sdgp_dtype)dtype,
+                              (int)std::min<int64_t>(top, INT32_MAX), floats(logprob), floats(entropy), floats(lse), floats(top_logprob),
+                              (int64_t*)data(top_token), s);
+  });
+}
+
+// logits, targets, lse, entropy, d_logprob, d_entropy, classes, n, m, scheme, seed, dtype, grad, values, meta
+ENTRY(token_logprob_backward) {
+  LmArgs in(args, nargs, 15);
+  const int dtype = nargs == 15 ? (int)PyLong_AsLong(args[11]) : 0;
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* logits = given(in, in.elements("logits", dtype), "logits");
+  int64_t rows = 0, K = 0;
+  if (in.ok) rows_and_k(logits, rows, K);
+  const at::Tensor* targets = given(in, in.of_type("targets", at::kLong, rows), "targets");
+  const at::Tensor* lse = given(in, in.of_type("lse", at::kFloat, rows), "lse");
+  const at::Tensor *entropy = in.of_type("entropy", at::kFloat, rows), *d_logprob = in.of_type("d_logprob", at::kFloat, rows),
+                   *d_entropy = in.of_type("d_entropy", at::kFloat, rows);
+  const int64_t classes = i64_or(in, K);
+  const int n = in.i32(), m = in.i32(), scheme = in.i32();
+  const uint64_t seed = in.u64();
+  in.i32();
+  const at::Tensor *grad = in.elements("grad", dtype), *values = in.elements("values", SDGP_BF16), *meta = in.elements("meta", SDGP_BF16);
+  in.same_numel("grad", grad, rows * K);
+  in.same_numel("values", values, rows * (K / 2));
+  in.same_numel("meta", meta, rows * (K / 16));
+  return status_on(in, [&](void* s) {
+    return sdgp_token_logprob_backward(data(logits), (const int64_t*)data(targets), floats(lse), floats(entropy), floats(d_logprob),
+                                       floats(d_entropy), rows, K, classes, n, m, (sdgp_scheme)scheme, seed, (sdgp_dtype)dtype, data(grad),
+                                       data(values), data(meta), s);
+  });
+}
+
 // Whether the C++ layers take a tensor: what Python hands over is an ordinary tensor (no subclass) in GPU memory of a 16-bit type, and
 // nothing watches or transforms the operators that run on it.
 bool plain_tensor(PyObject* o, int64_t dims) {
@@ -350,6 +483,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(prune), METHOD(relu_backward_prune), METHOD(maxpool_relu_backward_prune), METHOD(dgrad_linear),
                          METHOD(dgrad_linear_static), METHOD(dgrad_conv2d), METHOD(spmm_linear), METHOD(spmm_conv2d),
+                         METHOD(token_logprob), METHOD(token_logprob_backward),
                          METHOD(workspace_size_linear), METHOD(workspace_size_conv2d), METHOD(linear_layer),
                          METHOD(conv2d_layer), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sdgp_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

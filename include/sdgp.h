@@ -243,6 +243,34 @@ sdgp_status sdgp_token_logprob_backward(const void* logits, const int64_t* targe
                                         int m, sdgp_scheme scheme, uint64_t seed, sdgp_dtype dtype, void* grad, void* values, void* meta,
                                         void* stream);
 
+/* The boundary between two blocks of a residual network of linear layers: the norm behind a block, its gate and the residual scale, the
+ * sum, and the norm before the next block, in one pass. With rstd(v) = 1 / sqrt(mean(v^2) + eps) over a row:
+ *   n   = branch * rstd(branch) * post_weight      (post_weight null: n = branch)
+ *   out = alpha * residual + gate * n              (gate null: 1)
+ *   y   = out * rstd(out) * pre_weight             (pre_weight null: no y)
+ * branch, residual, out, y [rows, C]; post_weight, pre_weight [C]; gate [groups, C] with rows % groups == 0: row r takes gate
+ * r / (rows / groups) (1: the same for all, rows: one each, else one for each sequence). y is formed from the sums in fp32, before `out` is
+ * rounded. post_rstd, pre_rstd [rows] f32: what the backward pass wants; each optional. `out` may be `residual` or `branch` itself.
+ * Any C up to 2^24, any rows up to 2^28; all tensors of element type `dtype` 16-byte aligned (their rows need not be). */
+sdgp_status sdgp_residual_norm(const void* branch, const void* residual, const void* post_weight, const void* gate, const void* pre_weight,
+                               int64_t rows, int64_t C, int64_t groups, float alpha, float eps, sdgp_dtype dtype, void* out, void* y,
+                               float* post_rstd, float* pre_rstd, void* stream);
+
+/* Its gradient. d_out and d_y [rows, C] are the gradients that arrive on the residual stream and at y; either may be null (zero). With
+ * d_y, `out`, pre_rstd and pre_weight of the forward pass are needed; with post_weight, post_rstd is.
+ *   d_residual, d_branch [rows, C]     d_residual may be d_out itself
+ *   values, meta                       compressed pruned copy of d_branch - the dL/dO of the block's last layer -, as sdgp_prune (16-bit
+ *                                      types, n <= 2, C % m == 0, C % 16 == 0); n, m, scheme and seed are only looked at with them
+ *   d_gate [groups, C], d_post_weight, d_pre_weight [C]   f32, summed over rows in a fixed order
+ * each optional. Workspace: sdgp_workspace_size_residual_norm_backward() bytes, 256-byte aligned; asked for even where no sums are. */
+size_t sdgp_workspace_size_residual_norm_backward(int64_t rows, int64_t C, int64_t groups);
+sdgp_status sdgp_residual_norm_backward(const void* branch, const void* out, const void* d_out, const void* d_y, const void* post_weight,
+                                        const void* gate, const void* pre_weight, const float* post_rstd, const float* pre_rstd,
+                                        int64_t rows, int64_t C, int64_t groups, float alpha, int n, int m, sdgp_scheme scheme,
+                                        uint64_t seed, sdgp_dtype dtype, void* d_residual, void* d_branch, float* d_gate,
+                                        float* d_post_weight, float* d_pre_weight, void* values, void* meta, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
 /* Data gradient of a GROUPED convolution (the 3x3 convolutions of RegNetX, one of the networks of Section 4; the
  * contraction is Section 2.1 / Fig. 2 and Section 3.1 / Fig. 3 with the sum over output channels restricted to the
  * group of the input channel): output channel co belongs to group co / (Cout/groups) and is connected to the

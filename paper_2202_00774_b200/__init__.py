@@ -6,4 +6,5 @@ from .binding import (BF16, FP16, FP32, FLAG_CHANNEL, FLAG_DENSE, FLAG_FUSED, FL
                       sdgp_spmm_linear_typed, sdgp_spmm_conv2d_typed, sdgp_channel_scales, sdgp_relu_backward_prune, sdgp_residual_relu_backward_prune, sdgp_maxpool_relu_backward_prune, sdgp_workspace_size_conv2d,
                       sdgp_workspace_size_conv2d_grouped, sdgp_dgrad_conv2d_grouped,
                       sdgp_token_logprob, sdgp_token_logprob_backward,
+                      sdgp_residual_norm, sdgp_residual_norm_backward, sdgp_workspace_size_residual_norm_backward,
                       sdgp_workspace_size_linear, status_string)

@@ -24,6 +24,7 @@ EXPORTS = ["sdgp_prune", "sdgp_dgrad_linear", "sdgp_dgrad_conv2d", "sdgp_spmm_li
            "sdgp_workspace_size_linear", "sdgp_workspace_size_conv2d", "sdgp_workspace_size_conv2d_grouped",
            "sdgp_dgrad_conv2d_grouped", "sdgp_last_device_error",
            "sdgp_token_logprob", "sdgp_token_logprob_backward",
+           "sdgp_residual_norm", "sdgp_residual_norm_backward", "sdgp_workspace_size_residual_norm_backward",
            "sdgp_status_string"]
 
 _lib = None
@@ -96,6 +97,13 @@ def lib() -> ctypes.CDLL:
         L.sdgp_token_logprob.restype = i32
         L.sdgp_token_logprob_backward.argtypes = [vp] * 6 + [i64, i64, i64, i32, i32, i32, u64, i32, vp, vp, vp, vp]
         L.sdgp_token_logprob_backward.restype = i32
+        f32 = ctypes.c_float
+        L.sdgp_residual_norm.argtypes = [vp] * 5 + [i64, i64, i64, f32, f32, i32, vp, vp, vp, vp, vp]
+        L.sdgp_residual_norm.restype = i32
+        L.sdgp_workspace_size_residual_norm_backward.argtypes = [i64, i64, i64]
+        L.sdgp_workspace_size_residual_norm_backward.restype = sz
+        L.sdgp_residual_norm_backward.argtypes = [vp] * 9 + [i64, i64, i64, f32, i32, i32, i32, u64, i32] + [vp] * 8 + [sz, vp]
+        L.sdgp_residual_norm_backward.restype = i32
         L.sdgp_status_string.argtypes = [i32]
         L.sdgp_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -270,6 +278,30 @@ def sdgp_token_logprob_backward(logits, targets, lse, d_logprob, grad=None, entr
     ``values`` and ``meta`` its compressed pruned copy, in one pass."""
     _check((_torch or _load()).token_logprob_backward(logits, targets, lse, entropy, d_logprob, d_entropy, classes, n, m, scheme, seed,
                                                       dtype, grad, values, meta), "sdgp_token_logprob_backward")
+
+
+def sdgp_residual_norm(branch, residual, out, y=None, post_weight=None, gate=None, pre_weight=None, alpha=1.0, eps=1e-6, dtype=BF16,
+                       post_rstd=None, pre_rstd=None):
+    """``sdgp_residual_norm``: ``out`` = alpha * residual + gate * norm(branch) and ``y`` = norm(out), the boundary between two blocks.
+    The last dimension of ``branch`` is C; ``gate`` holds groups * C elements (one gate for each of `groups` equal runs of rows).
+    Outputs are caller-allocated; ``out`` may be ``residual`` or ``branch`` itself."""
+    _check((_torch or _load()).residual_norm(branch, residual, post_weight, gate, pre_weight, alpha, eps, dtype, out, y, post_rstd,
+                                             pre_rstd), "sdgp_residual_norm")
+
+
+def sdgp_workspace_size_residual_norm_backward(rows, C, groups=1) -> int:
+    return int(lib().sdgp_workspace_size_residual_norm_backward(rows, C, groups))
+
+
+def sdgp_residual_norm_backward(branch, out, d_out, d_y=None, post_weight=None, gate=None, pre_weight=None, post_rstd=None, pre_rstd=None,
+                                alpha=1.0, n=2, m=4, scheme=MAGNITUDE, seed=0, dtype=BF16, d_residual=None, d_branch=None, d_gate=None,
+                                d_post_weight=None, d_pre_weight=None, values=None, meta=None, workspace=None):
+    """``sdgp_residual_norm_backward``: the gradients of :func:`sdgp_residual_norm` from those at ``out`` and ``y``, with the
+    compressed pruned copy (``values``, ``meta``) of ``d_branch``, the dL/dO of the layer that gave ``branch``. Gradients of weights
+    and gate are float32. Outputs are caller-allocated (or None)."""
+    _check((_torch or _load()).residual_norm_backward(branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, alpha,
+                                                      n, m, scheme, seed, dtype, d_residual, d_branch, d_gate, d_post_weight,
+                                                      d_pre_weight, values, meta, workspace), "sdgp_residual_norm_backward")
 
 
 def sdgp_selftest_bounded_wait():

@@ -57,4 +57,58 @@ sdgp_status sdgp_token_logprob_backward(const void* logits, const int64_t* targe
                                                        (int)scheme, seed, (int)dtype, grad, values, meta, (cudaStream_t)stream));
 }
 
+static sdgp_status check_norm(int64_t rows, int64_t C, int64_t groups, sdgp_dtype dtype) {
+  if (!valid_dtype(dtype) || rows < 0 || C < 1 || groups < 1 || rows % groups != 0) return SDGP_ERR_INVALID_ARG;
+  if (rows > (int64_t)1 << 28 || C > (int64_t)1 << 24) return SDGP_ERR_UNSUPPORTED;
+  return SDGP_OK;
+}
+
+sdgp_status sdgp_residual_norm(const void* branch, const void* residual, const void* post_weight, const void* gate, const void* pre_weight,
+                               int64_t rows, int64_t C, int64_t groups, float alpha, float eps, sdgp_dtype dtype, void* out, void* y,
+                               float* post_rstd, float* pre_rstd, void* stream) {
+  const sdgp_status st = check_norm(rows, C, groups, dtype);
+  if (st != SDGP_OK || rows == 0) return st;
+  if (!branch || !residual || !out || (pre_weight && !y) || (!pre_weight && y)) return SDGP_ERR_INVALID_ARG;
+  for (const void* p : {branch, residual, post_weight, gate, pre_weight, (const void*)out, (const void*)y})
+    if (!aligned(p, 16)) return SDGP_ERR_ALIGNMENT;
+  if (!aligned(post_rstd, 4) || !aligned(pre_rstd, 4)) return SDGP_ERR_ALIGNMENT;
+  return status_of(sdgp::launch_residual_norm(branch, residual, post_weight, gate, pre_weight, rows, C, gate ? groups : 1, alpha, eps,
+                                              (int)dtype, out, y, post_rstd, pre_rstd, (cudaStream_t)stream));
+}
+
+size_t sdgp_workspace_size_residual_norm_backward(int64_t rows, int64_t C, int64_t groups) {
+  if (check_norm(rows, C, groups, SDGP_BF16) != SDGP_OK || rows == 0) return 0;
+  return (sdgp::residual_norm_backward_floats(rows, C, groups) * sizeof(float) + 255) / 256 * 256;
+}
+
+sdgp_status sdgp_residual_norm_backward(const void* branch, const void* out, const void* d_out, const void* d_y, const void* post_weight,
+                                        const void* gate, const void* pre_weight, const float* post_rstd, const float* pre_rstd,
+                                        int64_t rows, int64_t C, int64_t groups, float alpha, int n, int m, sdgp_scheme scheme,
+                                        uint64_t seed, sdgp_dtype dtype, void* d_residual, void* d_branch, float* d_gate,
+                                        float* d_post_weight, float* d_pre_weight, void* values, void* meta, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+  sdgp_status st = check_norm(rows, C, groups, dtype);
+  if (st == SDGP_OK) st = check_compressed(values, meta, C, n, m, (int)scheme, dtype);
+  if (st != SDGP_OK) return st;
+  if ((d_gate && !gate) || (d_post_weight && !post_weight) || (d_pre_weight && !pre_weight)) return SDGP_ERR_INVALID_ARG;
+  for (const float* p : {post_rstd, pre_rstd, (const float*)d_gate, (const float*)d_post_weight, (const float*)d_pre_weight})
+    if (!aligned(p, 4)) return SDGP_ERR_ALIGNMENT;
+  if (rows == 0) {  // sums over no rows
+    cudaError_t e = cudaSuccess;
+    for (float* p : {d_gate, d_post_weight, d_pre_weight})
+      if (p && e == cudaSuccess) e = cudaMemsetAsync(p, 0, (size_t)C * (p == d_gate ? (size_t)groups : 1) * sizeof(float), (cudaStream_t)stream);
+    return status_of(e);
+  }
+  if (!branch || (!d_out && !d_y) || (post_weight && !post_rstd)) return SDGP_ERR_INVALID_ARG;
+  if (d_y ? !out || !pre_weight || !pre_rstd : d_pre_weight != nullptr) return SDGP_ERR_INVALID_ARG;
+  for (const void* p : {branch, out, d_out, d_y, post_weight, gate, pre_weight, (const void*)d_residual, (const void*)d_branch})
+    if (!aligned(p, 16)) return SDGP_ERR_ALIGNMENT;
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < sdgp_workspace_size_residual_norm_backward(rows, C, groups))
+    return SDGP_ERR_WORKSPACE;
+  return status_of(sdgp::launch_residual_norm_backward(branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, rows, C,
+                                                       groups, alpha, n, m, (int)scheme, seed, (int)dtype, d_residual, d_branch, d_gate,
+                                                       d_post_weight, d_pre_weight, values, meta, (float*)workspace,
+                                                       (cudaStream_t)stream));
+}
+
 }  // extern "C"

@@ -1,0 +1,805 @@
+// The boundary between two blocks of a residual network of linear layers (a transformer's), and its gradient, sm_100a:
+//   n = b rstd(b) w_post      the norm behind a block whose last layer gave b (w_post absent: n = b)
+//   o = alpha r + g n         residual scale and gate
+//   y = o rstd(o) w_pre       the norm before the next block (w_pre absent: no y),      rstd(v) = 1 / sqrt(mean(v^2) + eps)
+// Backward, from gradients d_o and d_y, with u = o rstd(o), v = b rstd(b) (v = b without w_post) and means over a row:
+//   d = d_o + rstd(o) (w_pre d_y - u mean(w_pre d_y u)),   d_r = alpha d,   d_w_pre = sum over rows of d_y u
+//   d_b = rstd(b) (q - v mean(q v)),  q = d g w_post,      d_g = sum of d v w_post,  d_w_post = sum of d g v
+// d_b is the dL/dO of the block's last layer: like the producers below a ReLU the kernel writes it and its compressed pruned copy in one
+// pass.
+//
+// Both passes are bound by memory: 4 (backward 6) tensors are read or written once, rows stay in registers between the sums and their use.
+// TPR threads own a row, eight columns each, and go through rows at a fixed stride, so that sums over rows stay in registers as well.
+// A thread copies its own vectors of the next rows to shared memory asynchronously (nobody else reads them: no barrier), a row's sums
+// need one exchange between its warps.
+//
+// Rows of a width that is no multiple of eight start at any of eight places in a 16-byte vector. Ownership goes by the vectors of memory, not by
+// columns; the rows that one group of threads takes start at the same place (the strides are multiples of the period at which places
+// return), so a thread keeps its columns.
+#include "dgrad_common.cuh"
+#include "elements.cuh"
+
+namespace sdgp {
+namespace {
+
+constexpr int kMaxWarpsPerRow = 32;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {  // the rest of the 16 bytes is zeroed
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Threads of a CTA, and stages of the copies that are under way, for rows of TPR threads and A input tensors.
+template <int TPR>
+constexpr int kCtaThreads = TPR > 256 ? TPR : 256;
+template <int DT, int TPR, int A>
+struct Ring {
+  static constexpr int kChunk = kCtaThreads<TPR> * 16;               // 16 bytes of each thread side by side
+  static constexpr int kVec = kChunk * (Element<DT>::kBytes / 2);    // a vector: one chunk, or two of fp32
+  static constexpr int kStage = A * kVec;
+  static constexpr int kStages = kStage * 3 <= 100 * 1024 ? 3 : kStage * 2 <= 200 * 1024 ? 2 : 1;
+  static constexpr int kBytes = kStage * kStages;
+};
+
+// A thread's part of a row: eight elements of memory from element `first` of the row (negative in the row's first vector if the row does
+// not start on a vector), of which [lo, hi) are the row's.
+struct Part {
+  int first, lo, hi;
+  bool full;
+};
+__device__ __forceinline__ Part part_of(int64_t row, int C, int t) {
+  const int a = (int)((uint64_t)row * (uint64_t)C & 7u);
+  Part p;
+  p.first = t * 8 - a;
+  p.lo = t == 0 ? a : 0;
+  p.hi = max(0, min(8, C - p.first));
+  p.full = p.lo == 0 && p.hi == 8;
+  return p;
+}
+
+template <int DT, int CHUNK>
+__device__ __forceinline__ void copy_part(uint32_t dst, const void* src, int64_t row, int C, const Part& p) {
+  using E = Element<DT>;
+  const uint8_t* q = (const uint8_t*)src + (row * C + p.first) * E::kBytes;
+  const int bytes = p.hi * E::kBytes;
+  cp_async16(dst, q, (uint32_t)min(16, bytes));
+  if (E::k32) cp_async16(dst + CHUNK, bytes > 16 ? q + 16 : q, (uint32_t)max(0, bytes - 16));
+}
+template <int DT, int CHUNK>
+__device__ __forceinline__ void read_part(const uint8_t* at, const Part& p, float (&x)[8]) {
+  using E = Element<DT>;
+  typename E::Raw r;
+  r.a = *(const uint4*)at;
+  r.b = E::k32 ? *(const uint4*)(at + CHUNK) : make_uint4(0u, 0u, 0u, 0u);
+  E::widen(r, x);
+  if (!p.full) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < p.lo || e >= p.hi) x[e] = 0.0f;
+  }
+}
+template <int DT>
+__device__ __forceinline__ void write_part(void* dst, int64_t row, int C, const Part& p, const typename Element<DT>::Raw& r, const float (&x)[8]) {
+  using E = Element<DT>;
+  const int64_t at = row * C + p.first;
+  if (p.full) {
+    E::store8(dst, at, r);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= p.lo && e < p.hi) E::store(dst, at + e, x[e]);
+  }
+}
+// The thread's elements of a vector of C elements, as they are in memory; ones where there is no vector.
+template <int DT>
+__device__ __forceinline__ typename Element<DT>::Raw column_part(const void* src, int64_t offset, const Part& p) {
+  using E = Element<DT>;
+  if (src && p.full && ((offset + p.first) & 7) == 0) return E::load8(src, offset + p.first);
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = !src ? 1.0f : e >= p.lo && e < p.hi ? E::load(src, offset + p.first + e) : 0.0f;
+  return E::narrow(x);
+}
+__device__ __forceinline__ void write_sums(float* dst, const Part& p, const float (&x)[8]) {
+  if (p.full && ((uintptr_t)(dst + p.first) & 15u) == 0) {
+    *(float4*)(dst + p.first) = make_float4(x[0], x[1], x[2], x[3]);
+    *(float4*)(dst + p.first + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= p.lo && e < p.hi) dst[p.first + e] = x[e];
+  }
+}
+
+// Sums over the TPR threads of a row. `turn` alternates between two buffers, so one barrier a call is enough.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float* buffer, int slot, int& turn) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = warp_sum(s[i]);
+  if constexpr (TPR > 32) {
+    constexpr int W = TPR / 32;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x % TPR) >> 5;
+    float* b = buffer + (turn * (kCtaThreads<TPR> / TPR) + slot) * W * N;
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) b[i * W + warp] = s[i];
+    }
+    ptx::named_bar_sync(1 + slot, TPR);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = warp_sum(lane < W ? b[i * W + lane] : 0.0f);
+    turn ^= 1;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ forward
+
+struct NormParams {
+  const void *branch, *residual;  // [rows, C]
+  const void *post_weight, *gate, *pre_weight;  // [C], [groups, C], [C]; each optional
+  void *out, *y;
+  float *post_rstd, *pre_rstd;
+  int64_t rows, rows_per_group;
+  int C, groups;
+  float alpha, eps;
+};
+
+template <int DT, int TPR>
+__global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 512 ? 1 : 1024 / kCtaThreads<TPR>)
+norm_kernel(const NormParams p) {
+  using E = Element<DT>;
+  using R = Ring<DT, TPR, 2>;
+  constexpr int SLOTS = kCtaThreads<TPR> / TPR;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float buffer[2 * SLOTS * kMaxWarpsPerRow];
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const int64_t first = (int64_t)blockIdx.x * SLOTS + slot, stride = (int64_t)gridDim.x * SLOTS;
+  if (first >= p.rows) return;  // (a slot's threads share no barrier with the others)
+  const Part part = part_of(first, p.C, t);
+  uint8_t* mine = ring + threadIdx.x * 16;
+  const uint32_t mine_u32 = ptx::smem_u32(mine);
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < p.rows) {
+      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage, p.branch, row, p.C, part);
+      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + R::kVec, p.residual, row, p.C, part);
+    }
+    cp_async_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < R::kStages; ++s) fetch(first + s * stride, s);
+  const typename E::Raw w_post = column_part<DT>(p.post_weight, 0, part), w_pre = column_part<DT>(p.pre_weight, 0, part);
+  typename E::Raw gate = column_part<DT>(p.gate, 0, part);
+  const float inv_c = 1.0f / (float)p.C;
+  int stage = 0, turn = 0;
+  for (int64_t row = first; row < p.rows; row += stride) {
+    if (p.groups > 1) gate = column_part<DT>(p.gate, row / p.rows_per_group * p.C, part);
+    cp_async_wait<R::kStages - 1>();
+    float b[8], r[8], w[8], g[8];
+    read_part<DT, R::kChunk>(mine + stage * R::kStage, part, b);
+    read_part<DT, R::kChunk>(mine + stage * R::kStage + R::kVec, part, r);
+    E::widen(gate, g);
+    if (p.post_weight) {
+      float s[1] = {0.0f};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[0] = fmaf(b[e], b[e], s[0]);
+      row_sums<TPR>(s, buffer, slot, turn);
+      const float rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
+      if (t == 0 && p.post_rstd) p.post_rstd[row] = rstd;
+      E::widen(w_post, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] = b[e] * rstd * w[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = fmaf(g[e], b[e], p.alpha * r[e]);
+    write_part<DT>(p.out, row, p.C, part, E::narrow(r), r);
+    if (p.pre_weight) {  // (of the sums before their rounding to 16 bits)
+      float s[1] = {0.0f};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[0] = fmaf(r[e], r[e], s[0]);
+      row_sums<TPR>(s, buffer, slot, turn);
+      const float rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
+      if (t == 0 && p.pre_rstd) p.pre_rstd[row] = rstd;
+      E::widen(w_pre, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = r[e] * rstd * w[e];
+      write_part<DT>(p.y, row, p.C, part, E::narrow(r), r);
+    }
+    fetch(row + R::kStages * stride, stage);
+    if (++stage == R::kStages) stage = 0;
+  }
+  cp_async_wait<0>();
+}
+
+// ------------------------------------------------------------------------------------------------ backward
+
+struct NormGradParams {
+  const void *branch, *out, *d_out, *d_y;       // [rows, C]; d_out and d_y (then out as well) optional
+  const void *post_weight, *gate, *pre_weight;  // as in the forward pass; pre_weight only with d_y
+  const float *post_rstd, *pre_rstd;
+  void *d_residual, *d_branch;                  // [rows, C]; each optional
+  uint2* values;                                // compressed pruned copy of d_branch; each optional
+  uint8_t* meta;
+  float* d_gate;                                // [groups, C]; optional
+  // sums over the rows of one group of threads: [slots, C], or null where nobody asks for them; of the rows of one unit: [groups, gate_rows, C]
+  float *pre_sums, *post_sums, *gate_sums;
+  int64_t rows, rows_per_group;
+  int C, splits, units, gate_rows;  // gate_rows: units of a gate that have rows
+  float alpha;
+  int n, m, scheme;
+  uint32_t seed_lo, seed_hi;
+};
+
+// The pruning function as a call of its own: 24 forms, inlined into none of the kernels that use it (some 100 of their instructions per eight
+// elements, on a path that memory bounds).
+template <bool F16>
+__device__ __noinline__ uint4 prune_any(uint4 w, int64_t v, uint32_t seed_lo, uint32_t seed_hi, int n, int m, int scheme, int part) {
+  uint2 out = make_uint2(0u, 0u);
+  uint32_t pos = 0u;
+  KeepFlags k;
+#define SDGP_FORM(M, N)                                                                                                         \
+  if (m == M && n == N) {                                                                                                       \
+    const int l = part % (M <= 8 ? 1 : M / 8); /* the vector's place in a group that spans lanes */                             \
+    if (scheme == SDGP_RANDOM) compress_vector<M, N, SDGP_RANDOM, F16>(w, v, seed_lo, seed_hi, l, 0xFFFFFFFFu, out, pos, k);    \
+    else if (scheme == SDGP_MAGNITUDE) compress_vector<M, N, SDGP_MAGNITUDE, F16>(w, v, seed_lo, seed_hi, l, 0xFFFFFFFFu, out, pos, k); \
+    else compress_vector<M, N, SDGP_RESCALED_MAGNITUDE, F16>(w, v, seed_lo, seed_hi, l, 0xFFFFFFFFu, out, pos, k);              \
+  }
+  SDGP_FORM(4, 1) SDGP_FORM(4, 2) SDGP_FORM(8, 1) SDGP_FORM(8, 2) SDGP_FORM(16, 1) SDGP_FORM(16, 2) SDGP_FORM(32, 1) SDGP_FORM(32, 2)
+#undef SDGP_FORM
+  return make_uint4(out.x, out.y, pos >> 24, 0u);
+}
+
+// Rows are dealt out in units: rows of one gate, at a stride of `splits`. A slot takes units at the stride of all slots.
+template <int DT, int TPR, bool PRUNE>
+__global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 256 ? 1 : 2)
+norm_grad_kernel(const NormGradParams p) {
+  using E = Element<DT>;
+  using R = Ring<DT, TPR, 4>;
+  constexpr int SLOTS = kCtaThreads<TPR> / TPR;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float buffer[2 * 3 * SLOTS * kMaxWarpsPerRow];
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const int id = (int)blockIdx.x * SLOTS + slot, ids = (int)gridDim.x * SLOTS;
+  // rows of the walk: unit u = group * splits + s holds rows group * rows_per_group + s + i * splits
+  struct Walk {
+    int unit;
+    int64_t in_group;
+  };
+  auto row_of = [&](const Walk& w) { return (int64_t)(w.unit / p.splits) * p.rows_per_group + w.in_group; };
+  auto settle = [&](Walk& w) {  // to the first row at or behind w
+    while (w.unit < p.units && w.in_group >= p.rows_per_group) {
+      w.unit += ids;
+      w.in_group = w.unit % p.splits;
+    }
+  };
+  auto advance = [&](Walk& w) {
+    w.in_group += p.splits;
+    settle(w);
+  };
+  Walk here = {id, id % p.splits};
+  settle(here);
+  if (here.unit >= p.units) {
+    // no row at all: the sums of this slot are zero
+    const Part none = part_of(0, p.C, t);
+    const float zero[8] = {};
+    if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, none, zero);
+    if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, none, zero);
+  } else {
+    const Part part = part_of(row_of(here), p.C, t);
+    uint8_t* mine = ring + threadIdx.x * 16;
+    const uint32_t mine_u32 = ptx::smem_u32(mine);
+    auto fetch = [&](const Walk& w, int stage) {
+      if (w.unit < p.units) {
+        const int64_t row = row_of(w);
+        const uint32_t at = mine_u32 + stage * R::kStage;
+        copy_part<DT, R::kChunk>(at, p.branch, row, p.C, part);
+        if (p.d_out) copy_part<DT, R::kChunk>(at + R::kVec, p.d_out, row, p.C, part);
+        if (p.d_y) {
+          copy_part<DT, R::kChunk>(at + 2 * R::kVec, p.out, row, p.C, part);
+          copy_part<DT, R::kChunk>(at + 3 * R::kVec, p.d_y, row, p.C, part);
+        }
+      }
+      cp_async_commit();
+    };
+    Walk ahead = here;
+#pragma unroll
+    for (int s = 0; s < R::kStages; ++s) {
+      fetch(ahead, s);
+      if (ahead.unit < p.units) advance(ahead);
+    }
+    const typename E::Raw w_post = column_part<DT>(p.post_weight, 0, part), w_pre = column_part<DT>(p.pre_weight, 0, part);
+    typename E::Raw gate = column_part<DT>(p.gate, 0, part);
+    int gate_group = 0;
+    const float inv_c = 1.0f / (float)p.C;
+    float pre_sum[8] = {}, post_sum[8] = {}, gate_sum[8] = {};
+    int stage = 0, turn = 0;
+    while (here.unit < p.units) {
+      const int64_t row = row_of(here);
+      const int group = here.unit / p.splits;
+      if (p.gate && group != gate_group) {
+        gate = column_part<DT>(p.gate, (int64_t)group * p.C, part);
+        gate_group = group;
+      }
+      cp_async_wait<R::kStages - 1>();
+      const uint8_t* at = mine + stage * R::kStage;
+      float v[8], d[8], u[8], q[8], w[8];
+      read_part<DT, R::kChunk>(at, part, v);
+      if (p.d_out) {
+        read_part<DT, R::kChunk>(at + R::kVec, part, d);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = 0.0f;
+      }
+      if (p.post_weight) {
+        const float rstd = p.post_rstd[row];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= rstd;
+      }
+      // q = g w_post, the factor from d to the normalised branch's gradient
+      E::widen(gate, q);
+      E::widen(w_post, w);
+      if (p.post_weight) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] *= w[e];
+      }
+      // The two means of the formulas hang on each other: mean(q d v) needs d, which needs mean(w_pre d_y u). Written out,
+      //   sum q d v = sum q v (d_o + rstd w_pre d_y) - rstd mean(w_pre d_y u) sum q v u,
+      // so one exchange of three sums does.
+      float s[3] = {0.0f, 0.0f, 0.0f};
+      float rstd = 0.0f;
+      if (p.d_y) {
+        rstd = p.pre_rstd[row];
+        float dy[8];
+        read_part<DT, R::kChunk>(at + 2 * R::kVec, part, u);
+        read_part<DT, R::kChunk>(at + 3 * R::kVec, part, dy);
+        E::widen(w_pre, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          u[e] *= rstd;
+          pre_sum[e] = fmaf(dy[e], u[e], pre_sum[e]);
+          const float wd = dy[e] * w[e];
+          s[0] = fmaf(wd, u[e], s[0]);
+          d[e] = fmaf(rstd, wd, d[e]);
+          s[2] = fmaf(q[e] * v[e], u[e], s[2]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[1] = fmaf(q[e] * v[e], d[e], s[1]);
+      if (p.d_y || p.post_weight) row_sums<TPR>(s, buffer, slot, turn);
+      const float k = rstd * (s[0] * inv_c);
+      const float mean = (s[1] - k * s[2]) * inv_c;
+      float out[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        d[e] = fmaf(-k, u[e], d[e]);
+        out[e] = p.alpha * d[e];
+      }
+      if (p.d_residual) write_part<DT>(p.d_residual, row, p.C, part, E::narrow(out), out);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) gate_sum[e] = fmaf(d[e], v[e], gate_sum[e]);
+      if (p.post_weight) {
+        const float rstd_b = p.post_rstd[row];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = rstd_b * fmaf(q[e], d[e], -v[e] * mean);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = q[e] * d[e];
+      }
+      const typename E::Raw packed = E::narrow(out);
+      if (p.d_branch) write_part<DT>(p.d_branch, row, p.C, part, packed, out);
+      if constexpr (PRUNE) {  // (rows of whole groups of 16: every part is full or empty, and a group's lanes alike)
+        const int64_t vec = row * (p.C / 8) + t;
+        const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, t & 3);
+        if (part.full) {
+          if (p.values) p.values[vec] = make_uint2(c.x, c.y);
+          if (p.meta) p.meta[vec] = (uint8_t)c.z;
+        }
+      }
+      const Walk last = here;
+      advance(here);
+      if (here.unit != last.unit) {  // the unit's rows are done: sum of d v over them
+        E::widen(gate, q);
+        E::widen(w_post, w);
+        float g[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          post_sum[e] = fmaf(q[e], gate_sum[e], post_sum[e]);
+          g[e] = p.post_weight ? w[e] * gate_sum[e] : gate_sum[e];
+          gate_sum[e] = 0.0f;
+        }
+        if (p.gate_sums) write_sums(p.gate_sums + ((int64_t)group * p.gate_rows + last.unit % p.splits) * p.C, part, g);
+        else if (p.d_gate) write_sums(p.d_gate + (int64_t)group * p.C, part, g);
+      }
+      fetch(ahead, stage);
+      if (ahead.unit < p.units) advance(ahead);
+      if (++stage == R::kStages) stage = 0;
+    }
+    cp_async_wait<0>();
+    if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, part, pre_sum);
+    if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, part, post_sum);
+  }
+}
+
+// Sums of the slots' sums, in a fixed order. Job 0: d_pre_weight, 1: d_post_weight, 2 + g: gate g.
+struct SumParams {
+  const float *pre_sums, *post_sums, *gate_sums;
+  float *d_pre_weight, *d_post_weight, *d_gate;
+  int C, slots, gate_rows;
+};
+constexpr int kSumLanes = 16;
+__global__ void __launch_bounds__(32 * kSumLanes) norm_sums_kernel(const SumParams p) {
+  __shared__ float part[kSumLanes][33];
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  const int blocks_of_job = (p.C + 31) / 32, job = (int)(blockIdx.x / blocks_of_job), c = (int)(blockIdx.x % blocks_of_job) * 32 + threadIdx.x;
+  const float* src = job == 0 ? p.pre_sums : job == 1 ? p.post_sums : p.gate_sums + (int64_t)(job - 2) * p.gate_rows * p.C;
+  float* dst = job == 0 ? p.d_pre_weight : job == 1 ? p.d_post_weight : p.d_gate + (int64_t)(job - 2) * p.C;
+  if (!src) return;
+  const int n = job < 2 ? p.slots : p.gate_rows;
+  float s = 0.0f;
+  if (c < p.C)
+    for (int i = threadIdx.y; i < n; i += kSumLanes) s += src[(int64_t)i * p.C + c];
+  part[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.y == 0 && c < p.C) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kSumLanes; ++i) sum += part[i][threadIdx.x];
+    dst[c] = sum;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ rows wider than a CTA's registers
+//
+// One CTA a row, all vectors of it in turn; what a second pass needs again comes from the caches. The sums over rows are kept in the
+// slot's row of the workspace, each element by the thread that owns it.
+constexpr int kWideThreads = 1024;
+
+template <int DT>
+__device__ __forceinline__ void load_part(const void* src, int64_t row, int C, const Part& p, float (&x)[8]) {
+  using E = Element<DT>;
+  const int64_t at = row * C + p.first;
+  if (src && p.full) {
+    E::widen(E::load8(src, at), x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = src && e >= p.lo && e < p.hi ? E::load(src, at + e) : 0.0f;
+  }
+}
+template <int DT>
+__device__ __forceinline__ void load_columns(const void* src, int64_t offset, const Part& p, float (&x)[8]) {
+  Element<DT>::widen(column_part<DT>(src, offset, p), x);
+}
+__device__ __forceinline__ void add_sums(float* dst, const Part& p, const float (&x)[8], bool start) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e >= p.lo && e < p.hi) dst[p.first + e] = start ? x[e] : dst[p.first + e] + x[e];
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kWideThreads, 1) norm_wide_kernel(const NormParams p) {
+  using E = Element<DT>;
+  __shared__ float buffer[2 * kMaxWarpsPerRow];
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  const float inv_c = 1.0f / (float)p.C;
+  const int vectors = (p.C + 14) / 8, t = threadIdx.x;  // (at any place of the row's start)
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const int64_t gate_at = p.groups > 1 ? row / p.rows_per_group * p.C : 0;
+    float rstd_b = 1.0f;
+    if (p.post_weight) {
+      float s[1] = {0.0f};
+      for (int j = t; j < vectors; j += kWideThreads) {
+        float b[8];
+        load_part<DT>(p.branch, row, p.C, part_of(row, p.C, j), b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[0] = fmaf(b[e], b[e], s[0]);
+      }
+      row_sums<kWideThreads>(s, buffer, 0, turn);
+      rstd_b = rsqrtf(fmaf(s[0], inv_c, p.eps));
+      if (t == 0 && p.post_rstd) p.post_rstd[row] = rstd_b;
+    }
+    // (the output may lie in the place of an input: its sums are taken before anything is written, and formed again to be)
+    auto sums_of = [&](const Part& part, float (&o)[8]) {
+      float b[8], w[8], g[8];
+      load_part<DT>(p.branch, row, p.C, part, b);
+      load_part<DT>(p.residual, row, p.C, part, o);
+      load_columns<DT>(p.gate, gate_at, part, g);
+      load_columns<DT>(p.post_weight, 0, part, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(g[e], p.post_weight ? b[e] * rstd_b * w[e] : b[e], p.alpha * o[e]);
+    };
+    float rstd = 1.0f;
+    if (p.pre_weight) {
+      float s[1] = {0.0f};
+      for (int j = t; j < vectors; j += kWideThreads) {
+        float o[8];
+        sums_of(part_of(row, p.C, j), o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[0] = fmaf(o[e], o[e], s[0]);
+      }
+      row_sums<kWideThreads>(s, buffer, 0, turn);
+      rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
+      if (t == 0 && p.pre_rstd) p.pre_rstd[row] = rstd;
+    }
+    for (int j = t; j < vectors; j += kWideThreads) {
+      const Part part = part_of(row, p.C, j);
+      float o[8], w[8];
+      sums_of(part, o);
+      write_part<DT>(p.out, row, p.C, part, E::narrow(o), o);
+      if (p.pre_weight) {
+        load_columns<DT>(p.pre_weight, 0, part, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = o[e] * rstd * w[e];
+        write_part<DT>(p.y, row, p.C, part, E::narrow(o), o);
+      }
+    }
+  }
+}
+
+template <int DT, bool PRUNE>
+__global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const NormGradParams p) {
+  using E = Element<DT>;
+  __shared__ float buffer[2 * 3 * kMaxWarpsPerRow];
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  const float inv_c = 1.0f / (float)p.C;
+  const int vectors = (p.C + 14) / 8, rounds = (vectors + kWideThreads - 1) / kWideThreads, t = threadIdx.x;
+  int turn = 0;
+  bool first_row = true;
+  for (int unit = blockIdx.x; unit < p.units; unit += gridDim.x) {
+    const int group = unit / p.splits;
+    for (int64_t i = unit % p.splits; i < p.rows_per_group; i += p.splits) {
+      const int64_t row = group * p.rows_per_group + i;
+      const bool first_of_unit = i < p.splits;
+      const float rstd_b = p.post_weight ? p.post_rstd[row] : 1.0f, rstd = p.d_y ? p.pre_rstd[row] : 0.0f;
+      // v, u, q and d_o + rstd w_pre d_y of one vector, as in norm_grad_kernel
+      auto load_terms = [&](const Part& part, float (&v)[8], float (&u)[8], float (&q)[8], float (&d)[8], float (&wd)[8]) {
+        float w[8];
+        load_part<DT>(p.branch, row, p.C, part, v);
+        load_part<DT>(p.d_out, row, p.C, part, d);
+        load_columns<DT>(p.gate, (int64_t)group * p.C, part, q);
+        load_columns<DT>(p.post_weight, 0, part, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] *= rstd_b;
+          q[e] *= w[e];
+          u[e] = wd[e] = 0.0f;
+        }
+        if (p.d_y) {
+          load_part<DT>(p.out, row, p.C, part, u);
+          load_part<DT>(p.d_y, row, p.C, part, wd);
+          load_columns<DT>(p.pre_weight, 0, part, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            u[e] *= rstd;
+            wd[e] *= w[e];
+            d[e] = fmaf(rstd, wd[e], d[e]);
+          }
+        }
+      };
+      float s[3] = {0.0f, 0.0f, 0.0f};
+      for (int j = t; j < vectors; j += kWideThreads) {
+        const Part part = part_of(row, p.C, j);
+        float v[8], u[8], q[8], d[8], wd[8];
+        load_terms(part, v, u, q, d, wd);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          s[0] = fmaf(wd[e], u[e], s[0]);
+          s[1] = fmaf(q[e] * v[e], d[e], s[1]);
+          s[2] = fmaf(q[e] * v[e], u[e], s[2]);
+        }
+      }
+      row_sums<kWideThreads>(s, buffer, 0, turn);
+      const float k = rstd * (s[0] * inv_c), mean = (s[1] - k * s[2]) * inv_c;
+      for (int round = 0; round < rounds; ++round) {
+        const int j = t + round * kWideThreads;
+        const Part part = part_of(row, p.C, j);
+        float v[8], u[8], q[8], d[8], x[8], w[8];
+        load_terms(part, v, u, q, d, x);
+        if (p.pre_sums) {
+          load_part<DT>(p.d_y, row, p.C, part, x);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] *= u[e];
+          add_sums(p.pre_sums + (int64_t)blockIdx.x * p.C, part, x, first_row);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          d[e] = fmaf(-k, u[e], d[e]);
+          x[e] = p.alpha * d[e];
+        }
+        if (p.d_residual) write_part<DT>(p.d_residual, row, p.C, part, E::narrow(x), x);
+        if (p.post_sums) {
+          load_columns<DT>(p.gate, (int64_t)group * p.C, part, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = d[e] * v[e] * w[e];
+          add_sums(p.post_sums + (int64_t)blockIdx.x * p.C, part, x, first_row);
+        }
+        if (p.d_gate) {
+          load_columns<DT>(p.post_weight, 0, part, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = d[e] * v[e] * w[e];
+          add_sums(p.gate_sums ? p.gate_sums + ((int64_t)group * p.gate_rows + unit % p.splits) * p.C : p.d_gate + (int64_t)group * p.C, part, x, first_of_unit);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = p.post_weight ? rstd_b * fmaf(q[e], d[e], -v[e] * mean) : q[e] * d[e];
+        const typename E::Raw packed = E::narrow(x);
+        if (p.d_branch) write_part<DT>(p.d_branch, row, p.C, part, packed, x);
+        if constexpr (PRUNE) {
+          const int64_t vec = row * (p.C / 8) + j;
+          const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, j & 3);
+          if (part.full) {
+            if (p.values) p.values[vec] = make_uint2(c.x, c.y);
+            if (p.meta) p.meta[vec] = (uint8_t)c.z;
+          }
+        }
+      }
+      first_row = false;
+    }
+  }
+  if (first_row) {
+    const float zero[8] = {};
+    for (int j = t; j < vectors; j += kWideThreads) {
+      const Part none = part_of(0, p.C, j);
+      if (p.pre_sums) add_sums(p.pre_sums + (int64_t)blockIdx.x * p.C, none, zero, true);
+      if (p.post_sums) add_sums(p.post_sums + (int64_t)blockIdx.x * p.C, none, zero, true);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+int gcd8(int c) { return c % 8 == 0 ? 8 : c % 4 == 0 ? 4 : c % 2 == 0 ? 2 : 1; }
+
+// Threads of a row: the smallest power of two from 32 to 1024 whose vectors hold it at any place that it may start at; 0: the wide kernels.
+int threads_of_row(int64_t C) {
+  for (int t = 32; t <= 1024; t *= 2)
+    if (C + 8 - gcd8((int)(C % 8)) <= 8 * t) return t;
+  return 0;
+}
+
+struct Plan {
+  int tpr, slots_per_cta, ctas, period, splits, units, gate_rows;
+  int ids() const { return ctas * slots_per_cta; }
+};
+
+// How rows are dealt to slots (groups of threads). All rows of a slot start at the same place of a vector: they are multiples of the period
+// apart. groups == 0: the forward pass, rows at the stride of all slots.
+Plan plan_rows(int64_t rows, int64_t C, int64_t groups, int ctas_per_sm) {
+  Plan p = {};
+  p.tpr = threads_of_row(C);
+  p.slots_per_cta = p.tpr == 0 || p.tpr >= 256 ? 1 : 256 / p.tpr;
+  p.period = 8 / gcd8((int)(C % 8));
+  const int64_t most = (int64_t)sm_count() * ctas_per_sm;
+  const int64_t wanted = (rows + p.slots_per_cta - 1) / p.slots_per_cta;
+  int64_t ctas = wanted < most ? wanted : most;
+  if (groups == 0) {
+    if (ctas < wanted && p.period > p.slots_per_cta) ctas -= ctas % (p.period / p.slots_per_cta);
+    p.ctas = (int)ctas;
+    return p;
+  }
+  const int64_t per_group = rows / groups;
+  int64_t ids = ctas * p.slots_per_cta;
+  int64_t splits = ids / groups;
+  splits -= splits % p.period;
+  if (splits < p.period) splits = per_group == 1 || p.period == 1 ? 1 : p.period;
+  if (splits >= per_group) splits = (per_group + p.period - 1) / p.period * p.period;
+  if (per_group == 1) splits = 1;
+  p.splits = (int)splits;
+  p.units = (int)(groups * splits);
+  p.gate_rows = (int)(splits < per_group ? splits : per_group);
+  if (p.units > ids) {
+    // a slot takes several units: the first rows of two of them are ids / splits groups apart, or (splits == 1) ids groups
+    const int64_t multiple = splits == 1 ? p.period : (int64_t)p.period * splits;
+    const int64_t need = multiple > p.slots_per_cta ? multiple / p.slots_per_cta : 1;
+    ctas = ctas < need ? need : ctas - ctas % need;
+  } else {
+    ctas = (p.units + p.slots_per_cta - 1) / p.slots_per_cta;
+  }
+  p.ctas = (int)ctas;
+  return p;
+}
+
+constexpr int kForwardCtasPerSm(int tpr) { return tpr == 0 ? 2 : tpr > 512 ? 1 : tpr > 256 ? 2 : 4; }
+constexpr int kBackwardCtasPerSm(int tpr) { return tpr == 0 ? 1 : tpr > 256 ? 1 : 2; }
+
+template <auto Kernel, typename... Args>
+cudaError_t launch(int64_t ctas, dim3 block, int smem, cudaStream_t stream, const Args&... args) {
+  static bool done[kMaxDevices] = {};  // (what a kernel asks for is always the same)
+  const int dev = current_device();
+  if (dev < 0) return cudaErrorInvalidDevice;
+  if (smem > 0 && !done[dev]) {
+    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    done[dev] = true;
+  }
+  if (ctas > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, Kernel, args...);
+}
+
+template <int DT>
+cudaError_t launch_forward(const NormParams& p, const Plan& plan, cudaStream_t stream) {
+  switch (plan.tpr) {
+#define SDGP_ROW(T) \
+  case T: return launch<norm_kernel<DT, T>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 2>::kBytes, stream, p);
+    SDGP_ROW(32) SDGP_ROW(64) SDGP_ROW(128) SDGP_ROW(256) SDGP_ROW(512) SDGP_ROW(1024)
+#undef SDGP_ROW
+  }
+  return launch<norm_wide_kernel<DT>>(plan.ctas, dim3(kWideThreads), 0, stream, p);
+}
+
+template <int DT, bool PRUNE>
+cudaError_t launch_backward(const NormGradParams& p, const Plan& plan, cudaStream_t stream) {
+  switch (plan.tpr) {
+#define SDGP_ROW(T) \
+  case T: return launch<norm_grad_kernel<DT, T, PRUNE>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 4>::kBytes, stream, p);
+    SDGP_ROW(32) SDGP_ROW(64) SDGP_ROW(128) SDGP_ROW(256) SDGP_ROW(512) SDGP_ROW(1024)
+#undef SDGP_ROW
+  }
+  return launch<norm_grad_wide_kernel<DT, PRUNE>>(plan.ctas, dim3(kWideThreads), 0, stream, p);
+}
+
+Plan backward_plan(int64_t rows, int64_t C, int64_t groups) { return plan_rows(rows, C, groups, kBackwardCtasPerSm(threads_of_row(C))); }
+
+}  // namespace
+
+cudaError_t launch_residual_norm(const void* branch, const void* residual, const void* post_weight, const void* gate, const void* pre_weight,
+                                 int64_t rows, int64_t C, int64_t groups, float alpha, float eps, int dtype, void* out, void* y,
+                                 float* post_rstd, float* pre_rstd, cudaStream_t stream) {
+  const NormParams p = {branch, residual, post_weight, gate, pre_weight, out, y, post_rstd, pre_rstd, rows, rows / groups, (int)C, (int)groups,
+                        alpha, eps};
+  const Plan plan = plan_rows(rows, C, 0, kForwardCtasPerSm(threads_of_row(C)));
+  if (dtype == SDGP_BF16) return launch_forward<SDGP_BF16>(p, plan, stream);
+  if (dtype == SDGP_FP16) return launch_forward<SDGP_FP16>(p, plan, stream);
+  return launch_forward<SDGP_FP32>(p, plan, stream);
+}
+
+size_t residual_norm_backward_floats(int64_t rows, int64_t C, int64_t groups) {
+  const Plan plan = backward_plan(rows, C, groups);
+  return (size_t)C * (2 * (size_t)plan.ids() + (plan.splits > 1 ? (size_t)groups * plan.gate_rows : 0));
+}
+
+cudaError_t launch_residual_norm_backward(const void* branch, const void* out, const void* d_out, const void* d_y, const void* post_weight,
+                                          const void* gate, const void* pre_weight, const float* post_rstd, const float* pre_rstd,
+                                          int64_t rows, int64_t C, int64_t groups, float alpha, int n, int m, int scheme, uint64_t seed,
+                                          int dtype, void* d_residual, void* d_branch, float* d_gate, float* d_post_weight,
+                                          float* d_pre_weight, void* values, void* meta, float* workspace, cudaStream_t stream) {
+  const Plan plan = backward_plan(rows, C, groups);
+  float* pre_sums = d_pre_weight ? workspace : nullptr;
+  float* post_sums = d_post_weight ? workspace + (size_t)plan.ids() * C : nullptr;
+  float* gate_sums = d_gate && plan.splits > 1 ? workspace + 2 * (size_t)plan.ids() * C : nullptr;
+  const NormGradParams p = {branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, d_residual, d_branch,
+                            (uint2*)values, (uint8_t*)meta, d_gate, pre_sums, post_sums, gate_sums, rows, rows / groups, (int)C,
+                            plan.splits, plan.units, plan.gate_rows, alpha, n, m, scheme, (uint32_t)seed, (uint32_t)(seed >> 32)};
+  const bool prune = values || meta;
+  cudaError_t e;
+  if (dtype == SDGP_FP32) e = launch_backward<SDGP_FP32, false>(p, plan, stream);
+  else if (dtype == SDGP_BF16) e = prune ? launch_backward<SDGP_BF16, true>(p, plan, stream) : launch_backward<SDGP_BF16, false>(p, plan, stream);
+  else e = prune ? launch_backward<SDGP_FP16, true>(p, plan, stream) : launch_backward<SDGP_FP16, false>(p, plan, stream);
+  if (e != cudaSuccess || (!pre_sums && !post_sums && !gate_sums)) return e;
+  const SumParams q = {pre_sums, post_sums, gate_sums, d_pre_weight, d_post_weight, d_gate, (int)C, plan.ids(), plan.gate_rows};
+  const int64_t jobs = 2 + (gate_sums ? groups : 0);
+  return launch<norm_sums_kernel>(jobs * ((C + 31) / 32), dim3(32, kSumLanes), 0, stream, q);
+}
+
+}  // namespace sdgp

@@ -122,6 +122,17 @@ cudaError_t launch_token_logprob_backward(const void* logits, const int64_t* tar
                                           int m, int scheme, uint64_t seed, int dtype, void* grad, void* values, void* meta,
                                           cudaStream_t stream);
 
+// Norms around a block with gate and residual scale, and their gradient (norm.cu); null pointers and shapes as sdgp.h says.
+cudaError_t launch_residual_norm(const void* branch, const void* residual, const void* post_weight, const void* gate, const void* pre_weight,
+                                 int64_t rows, int64_t C, int64_t groups, float alpha, float eps, int dtype, void* out, void* y,
+                                 float* post_rstd, float* pre_rstd, cudaStream_t stream);
+size_t residual_norm_backward_floats(int64_t rows, int64_t C, int64_t groups);
+cudaError_t launch_residual_norm_backward(const void* branch, const void* out, const void* d_out, const void* d_y, const void* post_weight,
+                                          const void* gate, const void* pre_weight, const float* post_rstd, const float* pre_rstd,
+                                          int64_t rows, int64_t C, int64_t groups, float alpha, int n, int m, int scheme, uint64_t seed,
+                                          int dtype, void* d_residual, void* d_branch, float* d_gate, float* d_post_weight,
+                                          float* d_pre_weight, void* values, void* meta, float* workspace, cudaStream_t stream);
+
 // Launches a one-CTA kernel whose only wait can never be satisfied (50 ms limit).
 sdgp_status launch_bounded_wait_selftest(cudaStream_t stream);
 

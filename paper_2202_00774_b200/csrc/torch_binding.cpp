@@ -345,9 +345,21 @@ const at::Tensor* given(LmArgs& in, const at::Tensor* t, const char* name) {
   return t;
 }
 
+float f32(Args& in) {
+  if (!in.ok) return 0.0f;
+  const double v = PyFloat_AsDouble(*in.a++);
+  if (v == -1.0 && PyErr_Occurred()) in.ok = false;
+  return (float)v;
+}
+
+// The dtype argument (number `at`), read before the tensors whose elements it names.
+int dtype_argument(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t want, Py_ssize_t at) {
+  return nargs == want ? (int)PyLong_AsLong(args[at]) : 0;
+}
+
 ENTRY(token_logprob) {  // logits, targets, classes, dtype, logprob, entropy, lse, top_logprob, top_token
   LmArgs in(args, nargs, 9);
-  const int dtype = nargs == 9 ? (int)PyLong_AsLong(args[3]) : 0;
+  const int dtype = dtype_argument(args, nargs, 9, 3);
   if (PyErr_Occurred()) return nullptr;
   const at::Tensor* logits = given(in, in.elements("logits", dtype), "logits");
   int64_t rows = 0, K = 0;
@@ -376,7 +388,7 @@ ENTRY(token_logprob) {  // logits, targets, classes, dtype, logprob, entropy, ls
 // logits, targets, lse, entropy, d_logprob, d_entropy, classes, n, m, scheme, seed, dtype, grad, values, meta
 ENTRY(token_logprob_backward) {
   LmArgs in(args, nargs, 15);
-  const int dtype = nargs == 15 ? (int)PyLong_AsLong(args[11]) : 0;
+  const int dtype = dtype_argument(args, nargs, 15, 11);
   if (PyErr_Occurred()) return nullptr;
   const at::Tensor* logits = given(in, in.elements("logits", dtype), "logits");
   int64_t rows = 0, K = 0;
@@ -397,6 +409,73 @@ ENTRY(token_logprob_backward) {
     return sdgp_token_logprob_backward(data(logits), (const int64_t*)data(targets), floats(lse), floats(entropy), floats(d_logprob),
                                        floats(d_entropy), rows, K, classes, n, m, (sdgp_scheme)scheme, seed, (sdgp_dtype)dtype, data(grad),
                                        data(values), data(meta), s);
+  });
+}
+
+ENTRY(residual_norm) {  // branch, residual, post_weight, gate, pre_weight, alpha, eps, dtype, out, y, post_rstd, pre_rstd
+  LmArgs in(args, nargs, 12);
+  const int dtype = dtype_argument(args, nargs, 12, 7);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* branch = given(in, in.elements("branch", dtype), "branch");
+  int64_t rows = 0, C = 0;
+  if (in.ok) rows_and_k(branch, rows, C);
+  const at::Tensor* residual = given(in, in.elements("residual", dtype), "residual");
+  const at::Tensor *post_weight = in.elements("post_weight", dtype), *gate = in.elements("gate", dtype),
+                   *pre_weight = in.elements("pre_weight", dtype);
+  const float alpha = f32(in), eps = f32(in);
+  in.i32();
+  const at::Tensor* out = given(in, in.elements("out", dtype), "out");
+  const at::Tensor* y = in.elements("y", dtype);
+  const at::Tensor *post_rstd = in.of_type("post_rstd", at::kFloat, rows), *pre_rstd = in.of_type("pre_rstd", at::kFloat, rows);
+  in.same_numel("residual", residual, rows * C);
+  in.same_numel("out", out, rows * C);
+  in.same_numel("y", y, rows * C);
+  in.same_numel("post_weight", post_weight, C);
+  in.same_numel("pre_weight", pre_weight, C);
+  const int64_t groups = gate && C ? gate->numel() / C : 1;
+  in.same_numel("gate", gate, groups * C);
+  return status_on(in, [&](void* s) {
+    return sdgp_residual_norm(data(branch), data(residual), data(post_weight), data(gate), data(pre_weight), rows, C, groups, alpha, eps,
+                              (sdgp_dtype)dtype, data(out), data(y), floats(post_rstd), floats(pre_rstd), s);
+  });
+}
+
+// branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, alpha, n, m, scheme, seed, dtype, d_residual, d_branch, d_gate,
+// d_post_weight, d_pre_weight, values, meta, workspace
+ENTRY(residual_norm_backward) {
+  LmArgs in(args, nargs, 23);
+  const int dtype = dtype_argument(args, nargs, 23, 14);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* branch = given(in, in.elements("branch", dtype), "branch");
+  int64_t rows = 0, C = 0;
+  if (in.ok) rows_and_k(branch, rows, C);
+  const at::Tensor *out = in.elements("out", dtype), *d_out = in.elements("d_out", dtype), *d_y = in.elements("d_y", dtype);
+  const at::Tensor *post_weight = in.elements("post_weight", dtype), *gate = in.elements("gate", dtype),
+                   *pre_weight = in.elements("pre_weight", dtype);
+  const at::Tensor *post_rstd = in.of_type("post_rstd", at::kFloat, rows), *pre_rstd = in.of_type("pre_rstd", at::kFloat, rows);
+  const float alpha = f32(in);
+  const int n = in.i32(), m = in.i32(), scheme = in.i32();
+  const uint64_t seed = in.u64();
+  in.i32();
+  const at::Tensor *d_residual = in.elements("d_residual", dtype), *d_branch = in.elements("d_branch", dtype);
+  const int64_t groups = gate && C ? gate->numel() / C : 1;
+  const at::Tensor *d_gate = in.of_type("d_gate", at::kFloat, groups * C), *d_post_weight = in.of_type("d_post_weight", at::kFloat, C),
+                   *d_pre_weight = in.of_type("d_pre_weight", at::kFloat, C);
+  const at::Tensor *values = in.elements("values", SDGP_BF16), *meta = in.elements("meta", SDGP_BF16), *ws = in.on_device("workspace");
+  for (const auto& [name, t] : {std::pair<const char*, const at::Tensor*>{"out", out}, {"d_out", d_out}, {"d_y", d_y}, {"d_residual", d_residual},
+                                {"d_branch", d_branch}})
+    in.same_numel(name, t, rows * C);
+  in.same_numel("post_weight", post_weight, C);
+  in.same_numel("pre_weight", pre_weight, C);
+  in.same_numel("gate", gate, groups * C);
+  in.same_numel("values", values, rows * (C / 2));
+  in.same_numel("meta", meta, rows * (C / 16));
+  const size_t ws_bytes = ws ? (size_t)ws->nbytes() : 0;
+  return status_on(in, [&](void* s) {
+    return sdgp_residual_norm_backward(data(branch), data(out), data(d_out), data(d_y), data(post_weight), data(gate), data(pre_weight),
+                                       floats(post_rstd), floats(pre_rstd), rows, C, groups, alpha, n, m, (sdgp_scheme)scheme, seed,
+                                       (sdgp_dtype)dtype, data(d_residual), data(d_branch), floats(d_gate), floats(d_post_weight),
+                                       floats(d_pre_weight), data(values), data(meta), data(ws), ws_bytes, s);
   });
 }
 
@@ -483,7 +562,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(prune), METHOD(relu_backward_prune), METHOD(maxpool_relu_backward_prune), METHOD(dgrad_linear),
                          METHOD(dgrad_linear_static), METHOD(dgrad_conv2d), METHOD(spmm_linear), METHOD(spmm_conv2d),
-                         METHOD(token_logprob), METHOD(token_logprob_backward),
+                         METHOD(token_logprob), METHOD(token_logprob_backward), METHOD(residual_norm), METHOD(residual_norm_backward),
                          METHOD(workspace_size_linear), METHOD(workspace_size_conv2d), METHOD(linear_layer),
                          METHOD(conv2d_layer), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sdgp_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

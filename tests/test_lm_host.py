@@ -45,3 +45,47 @@ def logprob_backward(lib, logits=A, targets=A, lse=A, entropy=None, d_logprob=A,
     (OK, dict(grad=None)), (OK, dict(rows=0, logits=None, targets=None, lse=None, grad=None))])
 def test_logprob_backward(lib, status, change):
     assert logprob_backward(lib, **change) == status
+
+
+def norm(lib, branch=A, residual=A, post_weight=A, gate=A, pre_weight=A, rows=4, C=64, groups=1, dtype=BF16, out=A, y=A, post_rstd=None,
+         pre_rstd=None):
+    return lib.sdgp_residual_norm(branch, residual, post_weight, gate, pre_weight, rows, C, groups, 1.0, 1e-6, dtype, out, y, post_rstd,
+                                  pre_rstd, None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (INVALID, dict(dtype=3)), (INVALID, dict(rows=-1)), (INVALID, dict(C=0)), (INVALID, dict(groups=0)), (INVALID, dict(groups=3)),
+    (INVALID, dict(branch=None)), (INVALID, dict(residual=None)), (INVALID, dict(out=None)), (INVALID, dict(y=None)),
+    (INVALID, dict(pre_weight=None)), (UNSUPPORTED, dict(C=(1 << 24) + 1)), (UNSUPPORTED, dict(rows=(1 << 28) + 1)),
+    (ALIGNMENT, dict(branch=ODD)), (ALIGNMENT, dict(gate=ODD)), (ALIGNMENT, dict(y=ODD)), (ALIGNMENT, dict(pre_rstd=ODD)),
+    (OK, dict(rows=0, branch=None, residual=None, out=None, y=None))])
+def test_norm(lib, status, change):
+    assert norm(lib, **change) == status
+
+
+def norm_backward(lib, branch=A, out=A, d_out=A, d_y=A, post_weight=A, gate=A, pre_weight=A, post_rstd=A, pre_rstd=A, rows=4, C=64, groups=1,
+                  n=2, m=4, scheme=1, dtype=BF16, d_residual=A, d_branch=A, d_gate=A, d_post_weight=A, d_pre_weight=A, values=None, meta=None,
+                  workspace=A, size=None):
+    if size is None:
+        size = lib.sdgp_workspace_size_residual_norm_backward(rows, C, groups) if rows > 0 and C > 0 and groups > 0 else 1 << 20
+    return lib.sdgp_residual_norm_backward(branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, rows, C, groups, 1.0,
+                                           n, m, scheme, 0, dtype, d_residual, d_branch, d_gate, d_post_weight, d_pre_weight, values, meta,
+                                           workspace, size, None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (INVALID, dict(dtype=3)), (INVALID, dict(rows=-1)), (INVALID, dict(C=0)), (INVALID, dict(groups=3)), (INVALID, dict(branch=None)),
+    (INVALID, dict(d_out=None, d_y=None, d_pre_weight=None)), (INVALID, dict(out=None)), (INVALID, dict(pre_weight=None, d_pre_weight=None)),
+    (INVALID, dict(pre_rstd=None)), (INVALID, dict(post_rstd=None)), (INVALID, dict(gate=None)), (INVALID, dict(post_weight=None)),
+    (INVALID, dict(d_y=None)), (INVALID, dict(values=A, n=5)), (UNSUPPORTED, dict(values=A, n=3)), (UNSUPPORTED, dict(meta=A, dtype=FP32)),
+    (ALIGNMENT, dict(values=A, C=40, m=8)), (ALIGNMENT, dict(d_residual=ODD)), (ALIGNMENT, dict(d_gate=ODD)),
+    (WORKSPACE, dict(workspace=None)), (WORKSPACE, dict(workspace=ctypes.c_void_p(0x1010))), (WORKSPACE, dict(size=16))])
+def test_norm_backward(lib, status, change):
+    assert norm_backward(lib, **change) == status
+
+
+def test_norm_backward_workspace(lib):
+    size = lib.sdgp_workspace_size_residual_norm_backward
+    assert size(0, 64, 1) == 0 and size(4, 0, 1) == 0 and size(4, 64, 3) == 0
+    assert size(1, 64, 1) >= 2 * 64 * 4 and size(1 << 20, 4096, 1) < 1 << 24
+    assert size(30000, 1001, 10000) <= 30000 * 1001 * 4 + (1 << 24)   # sums of a gate for three rows each

@@ -271,6 +271,25 @@ sdgp_status sdgp_residual_norm_backward(const void* branch, const void* out, con
                                         float* d_post_weight, float* d_pre_weight, void* values, void* meta, void* workspace,
                                         size_t workspace_bytes, void* stream);
 
+/* Quantisation to 8 bits (e4m3: four exponent bits, three mantissa bits, largest number 448) with a scale for each block of 128 columns
+ * of one row (block_rows == 1: activations, gradients) or of 128 rows and columns (block_rows == 128: weights); the last block of a row or
+ * column may be smaller. x [rows, K] of element type `dtype`:
+ *   scale [ceil(rows / block_rows), ceil(K / 128)] f32   the power of two s with max|x| / s in (224, 448], at least 2^-126; 1 for a block of
+ *                                                       zeros, NaN for one that holds a NaN or an infinity
+ *   q     [rows, K] one byte each                       x / s rounded to the nearest e4m3 number, ties to even (NaN where s is)
+ * Requirements: K % 16 == 0; x and q 16-byte aligned. */
+sdgp_status sdgp_fp8_quantize(const void* x, int64_t rows, int64_t K, int block_rows, sdgp_dtype dtype, void* q, float* scale, void* stream);
+
+/* The product of two such matrices, the forward product of a fully connected layer in 8 bits:
+ *   y[r, f] = sum_b x_scale[r, b] * w_scale[f / 128, b] * sum_{k in block b} xq[r, k] * wq[f, k]
+ * xq [rows, K] with x_scale [rows, ceil(K / 128)], wq [features, K] with w_scale [ceil(features / 128), ceil(K / 128)] (any fp32 numbers),
+ * y [rows, features] of element type `dtype`. A block's products are summed on the tensor cores in fp32, blocks are scaled and added in fp32,
+ * y is rounded once. The data gradient dO . W is the same call with wq the quantised transpose of W.
+ * Requirements: K % 16 == 0; xq, wq and y 16-byte aligned; any rows and features. Where rows and features are few, the sum over K is
+ * split among multiprocessors; the order of all additions is fixed by the sizes. */
+sdgp_status sdgp_fp8_linear(const void* xq, const float* x_scale, const void* wq, const float* w_scale, void* y, int64_t rows,
+                            int64_t features, int64_t K, sdgp_dtype dtype, void* stream);
+
 /* Data gradient of a GROUPED convolution (the 3x3 convolutions of RegNetX, one of the networks of Section 4; the
  * contraction is Section 2.1 / Fig. 2 and Section 3.1 / Fig. 3 with the sum over output channels restricted to the
  * group of the input channel): output channel co belongs to group co / (Cout/groups) and is connected to the

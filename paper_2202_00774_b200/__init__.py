@@ -7,4 +7,5 @@ from .binding import (BF16, FP16, FP32, FLAG_CHANNEL, FLAG_DENSE, FLAG_FUSED, FL
                       sdgp_workspace_size_conv2d_grouped, sdgp_dgrad_conv2d_grouped,
                       sdgp_token_logprob, sdgp_token_logprob_backward,
                       sdgp_residual_norm, sdgp_residual_norm_backward, sdgp_workspace_size_residual_norm_backward,
+                      sdgp_fp8_quantize, sdgp_fp8_linear,
                       sdgp_workspace_size_linear, status_string)

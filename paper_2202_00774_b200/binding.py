@@ -25,6 +25,7 @@ EXPORTS = ["sdgp_prune", "sdgp_dgrad_linear", "sdgp_dgrad_conv2d", "sdgp_spmm_li
            "sdgp_dgrad_conv2d_grouped", "sdgp_last_device_error",
            "sdgp_token_logprob", "sdgp_token_logprob_backward",
            "sdgp_residual_norm", "sdgp_residual_norm_backward", "sdgp_workspace_size_residual_norm_backward",
+           "sdgp_fp8_quantize", "sdgp_fp8_linear",
            "sdgp_status_string"]
 
 _lib = None
@@ -104,6 +105,10 @@ def lib() -> ctypes.CDLL:
         L.sdgp_workspace_size_residual_norm_backward.restype = sz
         L.sdgp_residual_norm_backward.argtypes = [vp] * 9 + [i64, i64, i64, f32, i32, i32, i32, u64, i32] + [vp] * 8 + [sz, vp]
         L.sdgp_residual_norm_backward.restype = i32
+        L.sdgp_fp8_quantize.argtypes = [vp, i64, i64, i32, i32, vp, vp, vp]
+        L.sdgp_fp8_quantize.restype = i32
+        L.sdgp_fp8_linear.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i32, vp]
+        L.sdgp_fp8_linear.restype = i32
         L.sdgp_status_string.argtypes = [i32]
         L.sdgp_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -302,6 +307,18 @@ def sdgp_residual_norm_backward(branch, out, d_out, d_y=None, post_weight=None, 
     _check((_torch or _load()).residual_norm_backward(branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, alpha,
                                                       n, m, scheme, seed, dtype, d_residual, d_branch, d_gate, d_post_weight,
                                                       d_pre_weight, values, meta, workspace), "sdgp_residual_norm_backward")
+
+
+def sdgp_fp8_quantize(x, q, scale, block_rows=1, dtype=BF16):
+    """``sdgp_fp8_quantize``: ``x`` (last dimension K, a multiple of 16) to e4m3 numbers ``q`` (one byte an element) and their
+    float32 ``scale`` for each block of ``block_rows`` (1 or 128) rows and 128 columns."""
+    _check((_torch or _load()).fp8_quantize(x, q, scale, block_rows, dtype), "sdgp_fp8_quantize")
+
+
+def sdgp_fp8_linear(xq, x_scale, wq, w_scale, y, dtype=BF16):
+    """``sdgp_fp8_linear``: y [rows, features] = x . w^T for xq [rows, K] with a scale for each row and 128 columns, wq [features, K]
+    with a scale for each 128 x 128 block (e4m3 numbers, as :func:`sdgp_fp8_quantize` writes them)."""
+    _check((_torch or _load()).fp8_linear(xq, x_scale, wq, w_scale, y, dtype), "sdgp_fp8_linear")
 
 
 def sdgp_selftest_bounded_wait():

@@ -58,6 +58,15 @@ bool encode(CUtensorMap* tm, CUtensorMapDataType dt, int rank, const void* base,
       *tm = maps[i];
       return true;
     }
+  if (!encode_fresh(tm, dt, rank, base, dims, strides_bytes, box, swz)) return false;
+  const int slot = used < kMapCache ? used++ : (next = (next + 1) % kMapCache);
+  keys[slot] = key;
+  maps[slot] = *tm;
+  return true;
+}
+
+bool encode_fresh(CUtensorMap* tm, CUtensorMapDataType dt, int rank, const void* base, const uint64_t* dims,
+                  const uint64_t* strides_bytes, const uint32_t* box, CUtensorMapSwizzle swz) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint32_t ones[5] = {1, 1, 1, 1, 1};
@@ -71,9 +80,6 @@ bool encode(CUtensorMap* tm, CUtensorMapDataType dt, int rank, const void* base,
     const int dev = current_device();
     if (dev < 0 || cudaSetDevice(dev) != cudaSuccess || !make()) return false;
   }
-  const int slot = used < kMapCache ? used++ : (next = (next + 1) % kMapCache);
-  keys[slot] = key;
-  maps[slot] = *tm;
   return true;
 }
 
@@ -601,7 +607,7 @@ sdgp_status read_device_error() {
   if (cudaDeviceSynchronize() != cudaSuccess) return SDGP_ERR_CUDA;
   bool timed_out = false;
   cudaError_t (*const words[])(unsigned int*) = {take_error_word, take_error_general, take_error_halo_sparse, take_error_halo_dense,
-                                                 take_error_halo_fused, take_error_rows, take_error_grouped};
+                                                 take_error_halo_fused, take_error_rows, take_error_grouped, take_error_fp8};
   for (auto take : words) {
     unsigned int word = 0;
     if (take(&word) != cudaSuccess) return SDGP_ERR_CUDA;

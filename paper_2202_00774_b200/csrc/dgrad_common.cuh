@@ -34,6 +34,9 @@ struct DgradView {
 // Encodes a tiled tensor map, or takes it from the calling thread's cache. False: a driver call failed.
 bool encode(CUtensorMap* tm, CUtensorMapDataType dt, int rank, const void* base, const uint64_t* dims, const uint64_t* strides_bytes,
             const uint32_t* box, CUtensorMapSwizzle swz);
+// The same without the cache.
+bool encode_fresh(CUtensorMap* tm, CUtensorMapDataType dt, int rank, const void* base, const uint64_t* dims, const uint64_t* strides_bytes,
+                  const uint32_t* box, CUtensorMapSwizzle swz);
 // Ordinal of the current device, -1 if it cannot be asked or is not below kMaxDevices.
 constexpr int kMaxDevices = 64;
 int current_device();

@@ -111,4 +111,27 @@ sdgp_status sdgp_residual_norm_backward(const void* branch, const void* out, con
                                                        (cudaStream_t)stream));
 }
 
+sdgp_status sdgp_fp8_quantize(const void* x, int64_t rows, int64_t K, int block_rows, sdgp_dtype dtype, void* q, float* scale, void* stream) {
+  if (!valid_dtype(dtype) || rows < 0 || K < 0) return SDGP_ERR_INVALID_ARG;
+  if ((block_rows != 1 && block_rows != 128) || rows > 0x7FFFFFFF || K > 0x7FFFFFFF) return SDGP_ERR_UNSUPPORTED;
+  if (rows == 0 || K == 0) return SDGP_OK;
+  if (!x || !q || !scale) return SDGP_ERR_INVALID_ARG;
+  if (K % 16 != 0 || !aligned(x, 16) || !aligned(q, 16) || !aligned(scale, 4)) return SDGP_ERR_ALIGNMENT;
+  // (the grid: a CTA takes 64 blocks of rows, or one square)
+  const int64_t blocks = (K + 127) / 128;
+  if ((block_rows == 128 ? (rows + 127) / 128 * blocks : rows * blocks / 64) >= 0x7FFFFFFF) return SDGP_ERR_UNSUPPORTED;
+  return status_of(sdgp::launch_fp8_quantize(x, rows, K, block_rows, (int)dtype, q, scale, (cudaStream_t)stream));
+}
+
+sdgp_status sdgp_fp8_linear(const void* xq, const float* x_scale, const void* wq, const float* w_scale, void* y, int64_t rows,
+                            int64_t features, int64_t K, sdgp_dtype dtype, void* stream) {
+  if (!valid_dtype(dtype) || rows < 0 || features < 0 || K < 1) return SDGP_ERR_INVALID_ARG;
+  if (rows > 0x7FFFFF00 || features > 0x7FFFFF00 || K > 0x7FFFFF00) return SDGP_ERR_UNSUPPORTED;
+  if (rows == 0 || features == 0) return SDGP_OK;
+  if (!xq || !x_scale || !wq || !w_scale || !y) return SDGP_ERR_INVALID_ARG;
+  if (K % 16 != 0 || !aligned(xq, 16) || !aligned(wq, 16) || !aligned(y, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4))
+    return SDGP_ERR_ALIGNMENT;
+  return sdgp::launch_fp8_linear(xq, x_scale, wq, w_scale, y, rows, features, K, (int)dtype, (cudaStream_t)stream);
+}
+
 }  // extern "C"

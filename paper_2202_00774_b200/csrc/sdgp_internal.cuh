@@ -133,6 +133,12 @@ cudaError_t launch_residual_norm_backward(const void* branch, const void* out, c
                                           int dtype, void* d_residual, void* d_branch, float* d_gate, float* d_post_weight,
                                           float* d_pre_weight, void* values, void* meta, float* workspace, cudaStream_t stream);
 
+// Quantisation to e4m3 (fp8_quantize.cu; block_rows 1 or 128) and the product of two quantised matrices (fp8_linear.cu); K a multiple of 16.
+cudaError_t launch_fp8_quantize(const void* x, int64_t rows, int64_t K, int block_rows, int dtype, void* q, float* scale, cudaStream_t stream);
+sdgp_status launch_fp8_linear(const void* xq, const float* x_scale, const void* wq, const float* w_scale, void* y, int64_t rows,
+                              int64_t features, int64_t K, int dtype, cudaStream_t stream);
+cudaError_t take_error_fp8(unsigned int* word);
+
 // Launches a one-CTA kernel whose only wait can never be satisfied (50 ms limit).
 sdgp_status launch_bounded_wait_selftest(cudaStream_t stream);
 

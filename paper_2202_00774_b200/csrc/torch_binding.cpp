@@ -479,6 +479,55 @@ ENTRY(residual_norm_backward) {
   });
 }
 
+// A tensor of e4m3 numbers: one byte an element.
+const at::Tensor* bytes_of(LmArgs& in, const char* name) {
+  const at::Tensor* t = given(in, in.on_device(name), name);
+  if (t && t->element_size() != 1) in.fail(name, "must hold one byte an element (float8_e4m3fn or uint8)");
+  return t;
+}
+
+ENTRY(fp8_quantize) {  // x, q, scale, block_rows, dtype
+  LmArgs in(args, nargs, 5);
+  const int dtype = dtype_argument(args, nargs, 5, 4);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* x = given(in, in.elements("x", dtype), "x");
+  const at::Tensor* q = bytes_of(in, "q");
+  const at::Tensor* scale = given(in, in.of_type("scale", at::kFloat, -1), "scale");
+  const int block_rows = in.i32();
+  in.i32();
+  int64_t rows = 0, K = 0;
+  if (in.ok) {
+    rows_and_k(x, rows, K);
+    in.same_numel("q", q, rows * K);
+    if (block_rows > 0) in.same_numel("scale", scale, (rows + block_rows - 1) / block_rows * ((K + 127) / 128));
+  }
+  return status_on(in, [&](void* s) { return sdgp_fp8_quantize(data(x), rows, K, block_rows, (sdgp_dtype)dtype, data(q), floats(scale), s); });
+}
+
+ENTRY(fp8_linear) {  // xq, x_scale, wq, w_scale, y, dtype
+  LmArgs in(args, nargs, 6);
+  const int dtype = dtype_argument(args, nargs, 6, 5);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Tensor* xq = bytes_of(in, "xq");
+  const at::Tensor* x_scale = given(in, in.of_type("x_scale", at::kFloat, -1), "x_scale");
+  const at::Tensor* wq = bytes_of(in, "wq");
+  const at::Tensor* w_scale = given(in, in.of_type("w_scale", at::kFloat, -1), "w_scale");
+  const at::Tensor* y = given(in, in.elements("y", dtype), "y");
+  in.i32();
+  int64_t rows = 0, K = 0, features = 0, wk = 0;
+  if (in.ok) {
+    rows_and_k(wq, features, wk);
+    rows_and_k(xq, rows, K);
+    if (wk != K) in.fail("xq and wq", "must have the same last dimension");
+    in.same_numel("x_scale", x_scale, rows * ((K + 127) / 128));
+    in.same_numel("w_scale", w_scale, (features + 127) / 128 * ((K + 127) / 128));
+    in.same_numel("y", y, rows * features);
+  }
+  return status_on(in, [&](void* s) {
+    return sdgp_fp8_linear(data(xq), floats(x_scale), data(wq), floats(w_scale), data(y), rows, features, K, (sdgp_dtype)dtype, s);
+  });
+}
+
 // Whether the C++ layers take a tensor: what Python hands over is an ordinary tensor (no subclass) in GPU memory of a 16-bit type, and
 // nothing watches or transforms the operators that run on it.
 bool plain_tensor(PyObject* o, int64_t dims) {
@@ -563,6 +612,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 PyMethodDef methods[] = {METHOD(prune), METHOD(relu_backward_prune), METHOD(maxpool_relu_backward_prune), METHOD(dgrad_linear),
                          METHOD(dgrad_linear_static), METHOD(dgrad_conv2d), METHOD(spmm_linear), METHOD(spmm_conv2d),
                          METHOD(token_logprob), METHOD(token_logprob_backward), METHOD(residual_norm), METHOD(residual_norm_backward),
+                         METHOD(fp8_quantize), METHOD(fp8_linear),
                          METHOD(workspace_size_linear), METHOD(workspace_size_conv2d), METHOD(linear_layer),
                          METHOD(conv2d_layer), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sdgp_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -89,3 +89,29 @@ def test_norm_backward_workspace(lib):
     assert size(0, 64, 1) == 0 and size(4, 0, 1) == 0 and size(4, 64, 3) == 0
     assert size(1, 64, 1) >= 2 * 64 * 4 and size(1 << 20, 4096, 1) < 1 << 24
     assert size(30000, 1001, 10000) <= 30000 * 1001 * 4 + (1 << 24)   # sums of a gate for three rows each
+
+
+def quantize(lib, x=A, rows=4, K=64, block_rows=1, dtype=BF16, q=A, scale=A):
+    return lib.sdgp_fp8_quantize(x, rows, K, block_rows, dtype, q, scale, None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (INVALID, dict(dtype=3)), (INVALID, dict(rows=-1)), (INVALID, dict(K=-16)), (INVALID, dict(x=None)), (INVALID, dict(q=None)),
+    (INVALID, dict(scale=None)), (UNSUPPORTED, dict(block_rows=64)), (UNSUPPORTED, dict(rows=1 << 31)), (ALIGNMENT, dict(K=40)),
+    (ALIGNMENT, dict(x=ODD)), (ALIGNMENT, dict(q=ODD)), (ALIGNMENT, dict(scale=ODD)), (OK, dict(rows=0, x=None)), (OK, dict(K=0, x=None)),
+    (UNSUPPORTED, dict(rows=(1 << 31) - 1, K=(1 << 31) - 16))])
+def test_quantize(lib, status, change):
+    assert quantize(lib, **change) == status
+
+
+def linear(lib, xq=A, x_scale=A, wq=A, w_scale=A, y=A, rows=4, features=64, K=64, dtype=BF16):
+    return lib.sdgp_fp8_linear(xq, x_scale, wq, w_scale, y, rows, features, K, dtype, None)
+
+
+@pytest.mark.parametrize("status,change", [
+    (INVALID, dict(dtype=3)), (INVALID, dict(rows=-1)), (INVALID, dict(features=-1)), (INVALID, dict(K=0)), (INVALID, dict(xq=None)),
+    (INVALID, dict(x_scale=None)), (INVALID, dict(wq=None)), (INVALID, dict(w_scale=None)), (INVALID, dict(y=None)),
+    (UNSUPPORTED, dict(rows=1 << 31)), (ALIGNMENT, dict(K=40)), (ALIGNMENT, dict(xq=ODD)), (ALIGNMENT, dict(y=ODD)),
+    (ALIGNMENT, dict(w_scale=ODD)), (OK, dict(rows=0, xq=None)), (OK, dict(features=0, wq=None))])
+def test_fp8_linear(lib, status, change):
+    assert linear(lib, **change) == status

@@ -14,8 +14,6 @@
 namespace sdgp {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr float kLog2e = 1.4426950408889634f;
 // Below this difference of two logits the exponential is zero in fp32. Differences are cut off there, so that a masked logit
 // (-infinity, or the type's lowest value) gives the product 0 * (a number), never 0 * infinity.
@@ -41,52 +39,50 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
 
 // ---- the k <= 32 largest logits ----
 //
-// A warp keeps its 32 largest so far in descending order, one in each lane, as keys that order by value and, among equal values, by the
-// lower index first; 0 is the key of no element.
+// Keys order by value and, among equal values, by the lower index first; 0 is the key of no element. A CTA collects keys that reach a
+// bound below which k others are known to lie: to begin with, a value that k threads' largest elements reach; later, the k-th largest key
+// collected. With random logits 20 of 131072 leave some hundred keys to be sorted. (Lists kept sorted in each warp's registers, an insertion
+// at a time, took 26 us for one row of 131072 bf16 logits on a cluster of eight CTAs; 2.5 us of them without the alternatives.)
 using Key = unsigned long long;
 
-__device__ __forceinline__ Key make_key(float x, uint32_t index) {
+__device__ __forceinline__ uint32_t ordered(float x) {
   const uint32_t b = __float_as_uint(x + 0.0f);  // (-0 equals +0)
-  return ((Key)(b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u)) << 32) | (uint32_t)~index;
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ Key make_key(float x, uint32_t index) { return ((Key)ordered(x) << 32) | (uint32_t)~index; }
 __device__ __forceinline__ float key_value(Key k) {
   const uint32_t o = (uint32_t)(k >> 32);
   return __uint_as_float((o & 0x80000000u) ? o ^ 0x80000000u : ~o);
 }
 
-__device__ __forceinline__ Key larger(Key a, Key b) { return a > b ? a : b; }
-__device__ __forceinline__ Key smaller(Key a, Key b) { return a > b ? b : a; }
+constexpr int kMostKeys = 512;      // that a CTA collects
+constexpr int kSortAbove = 128;     // as many are sorted out: a higher bound lets fewer of what follows in
 
-// Sorts a bitonic sequence of 32 keys (one a lane) in descending order.
-__device__ __forceinline__ Key sort_bitonic(Key k, int lane) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    const Key o = __shfl_xor_sync(0xFFFFFFFFu, k, d);
-    k = (lane & d) ? smaller(k, o) : larger(k, o);
-  }
-  return k;
-}
-__device__ __forceinline__ Key sort32(Key k, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 32; size <<= 1) {
-#pragma unroll
-    for (int d = size >> 1; d > 0; d >>= 1) {
-      const Key o = __shfl_xor_sync(0xFFFFFFFFu, k, d);
-      const bool up = (lane & size) != 0 && size < 32;  // this part in ascending order
-      k = (((lane & d) != 0) != up) ? smaller(k, o) : larger(k, o);
+struct Candidates {
+  Key keys[kMostKeys];
+  Key best[32];
+  uint32_t bound[8];
+  int count;
+};
+
+// The `top` largest of the first n keys to c.best in descending order (fewer: zeros behind them). Keys of elements all
+// differ, so a key's place is the number of larger ones. All threads of the CTA; ends with a barrier.
+template <int NT>
+__device__ __forceinline__ void sort_out(Candidates& c, int n, int top) {
+  if (threadIdx.x < 32) c.best[threadIdx.x] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const Key k = c.keys[i];
+    int place = 0;
+    int j = 0;
+    for (; j + 2 <= n; j += 2) {
+      const ulonglong2 o = *(const ulonglong2*)&c.keys[j];
+      place += (o.x > k) + (o.y > k);
     }
+    if (j < n) place += c.keys[j] > k;
+    if (place < top) c.best[place] = k;
   }
-  return k;
-}
-// The 32 largest of two descending lists.
-__device__ __forceinline__ Key merge_lists(Key a, Key b, int lane) {
-  return sort_bitonic(larger(a, __shfl_sync(0xFFFFFFFFu, b, 31 - lane)), lane);
-}
-// One more key (the same in all lanes) into a descending list.
-__device__ __forceinline__ Key insert(Key list, Key k, int lane) {
-  const int place = __popc(__ballot_sync(0xFFFFFFFFu, list > k));
-  const Key up = __shfl_up_sync(0xFFFFFFFFu, list, 1);
-  return lane < place ? list : lane == place ? k : up;
+  __syncthreads();
 }
 
 struct LogprobParams {
@@ -100,19 +96,22 @@ struct LogprobParams {
 };
 
 constexpr int kUnroll = 4;  // vectors of eight elements a thread has in flight
+constexpr int kMostParts = 8;
 
 // A cluster of CTAs (one where there are rows enough for all multiprocessors) reads a row in slices; its first CTA joins what the others found
 // through distributed shared memory.
-template <int DT, bool TOP>
-__global__ void __launch_bounds__(kThreads)
+template <int DT, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, NT == 32 ? 24 : 1024 / NT)
 logprob_kernel(const LogprobParams p) {
   using E = Element<DT>;
+  constexpr int kWarps = NT / 32;
   __shared__ Stats stats[kWarps];
-  __shared__ Key lists[TOP ? kWarps : 1][32];
+  __shared__ __align__(16) Candidates found[1];
+  Candidates& c = found[0];
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t parts = ptx::cluster_nctarank(), part = ptx::cluster_ctarank();
+  const uint32_t parts = NT == 32 ? 1u : ptx::cluster_nctarank(), part = NT == 32 ? 0u : ptx::cluster_ctarank();
   const int64_t row = blockIdx.x / parts;
   const uint8_t* base = (const uint8_t*)p.logits + row * p.K * E::kBytes;
   // elements up to the row's first 16-byte boundary, whole vectors of eight, the rest
@@ -121,171 +120,172 @@ logprob_kernel(const LogprobParams p) {
   const int tail0 = head + nvec * 8;
   const void* body = base + (int64_t)head * E::kBytes;
 
-  Stats st = {-INFINITY, 0.0f, 0.0f};
-  Key list = 0;
-  float floor_value = 0.0f;  // the k-th largest so far; nothing at or below it enters (what is read later has a higher index)
-  bool full = false;
+  float m = -INFINITY;
+  float2 s = {0.0f, 0.0f}, t = {0.0f, 0.0f};  // sums of even and of odd elements
+  Key bound = 0;
+  int held = 0;  // keys of the rounds before
+  if (TOP && threadIdx.x == 0) c.count = 0;
 
-  const int stride = (int)parts * kThreads;
-  for (int v0 = (int)part * kThreads + warp * 32; v0 < nvec; v0 += stride * kUnroll) {
+  // the CTA's slice, a round of it at a time (the same number of rounds in all its warps: the candidates meet at barriers)
+  const int stride = (int)parts * NT, first = (int)part * NT;
+  const int rounds = nvec > first ? (nvec - first + stride * kUnroll - 1) / (stride * kUnroll) : 0;
+  for (int round = 0; round < rounds; ++round) {
+    const int v0 = first + round * stride * kUnroll + (int)threadIdx.x;
     typename E::Raw raw[kUnroll];
-    int live = 0;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) raw[u] = v0 + u * stride < nvec ? E::load8(body, (int64_t)(v0 + u * stride) * 8) : E::lowest8();
+    float x[kUnroll][8];
+    float most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int v = v0 + lane + u * stride;
-      if (v < nvec) {
-        raw[u] = E::load8(body, (int64_t)v * 8);
-        live = u + 1;
+      E::widen(raw[u], x[u]);
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) most = fmaxf(most, fmaxf(x[u][e], x[u][e + 1]));
+    }
+    {
+      const float old = m;
+      m = fmaxf(m, most);
+      const float ref = finite_reference(m), ds = max_nan(old - ref, kFarBelow), f = exp2_approx(ds * kLog2e);
+      const float2 f2 = {f, f}, ds2 = {ds, ds}, minus_ref = {-ref, -ref}, log2e = {kLog2e, kLog2e};
+      t = mul2(f2, fma2(s, ds2, t));
+      s = mul2(s, f2);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          float2 d = add2({x[u][e], x[u][e + 1]}, minus_ref);
+          d = {max_nan(d.x, kFarBelow), max_nan(d.y, kFarBelow)};
+          float2 w = mul2(d, log2e);
+          w = {exp2_approx(w.x), exp2_approx(w.y)};
+          s = add2(s, w);
+          t = fma2(w, d, t);
+        }
       }
     }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float x[8];
-      E::widen(raw[u], x);
-      const bool on = u < live;
-      float most = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, x[e]);
-      if (on) {
-        const float m = fmaxf(st.m, most), ref = finite_reference(m);
-        const float ds = max_nan(st.m - ref, kFarBelow), f = exp2_approx(ds * kLog2e);
-        st.t = f * (st.t + st.s * ds);
-        st.s *= f;
-        st.m = m;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float d = max_nan(x[e] - ref, kFarBelow), w = exp2_approx(d * kLog2e);
-          st.s += w;
-          st.t = fmaf(w, d, st.t);
+    if constexpr (TOP) {
+      if (round == 0) {
+        // ceil(top / warps) lanes of each warp that has elements reach the warp's bound, so `top` elements reach the least of them
+        const int with = min(kWarps, (nvec - first + 31) / 32), each = (p.top + with - 1) / with;
+        uint32_t mine = v0 < nvec ? ordered(most) : 0u, reached = 0u;
+        for (int i = 0; i < each; ++i) {
+          reached = __reduce_max_sync(0xFFFFFFFFu, mine);
+          if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, mine == reached)) - 1) mine = 0u;
         }
+        if (lane == 0) c.bound[warp] = reached;
+        __syncthreads();
+        reached = 0xFFFFFFFFu;
+        for (int w = 0; w < with; ++w) reached = min(reached, c.bound[w]);
+        bound = (Key)reached << 32;
       }
-      if (TOP) {
-        if (!__any_sync(0xFFFFFFFFu, on && (!full || most > floor_value))) continue;
-        const uint32_t i0 = (uint32_t)(head + (v0 + lane + u * stride) * 8);
-        uint32_t mask = 0;
-        if (!full) {
-          // the largest of each lane start the list
-          Key best = 0;
+      for (;;) {
+        const float least = bound ? key_value(bound) : -INFINITY;
+        bool added = false;
+        if (most >= least) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (on && x[e] == x[e]) best = larger(best, make_key(x[e], i0 + e));
-          list = merge_lists(list, sort32(best, lane), lane);
-          const Key kth = __shfl_sync(0xFFFFFFFFu, list, p.top - 1);
-          full = kth != 0;
-          if (full) floor_value = key_value(kth);
-          // (an element equal to the k-th may have a lower index here: the comparison of keys decides)
+          for (int u = 0; u < kUnroll; ++u) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (on && x[e] == x[e] && (!full || x[e] >= floor_value) && make_key(x[e], i0 + e) != best) mask |= 1u << e;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (on && x[e] > floor_value) mask |= 1u << e;
-        }
-        Key kth = __shfl_sync(0xFFFFFFFFu, list, p.top - 1);
-        for (;;) {
-          const uint32_t lanes = __ballot_sync(0xFFFFFFFFu, mask != 0);
-          if (lanes == 0) break;
-          const int src = __ffs(lanes) - 1;
-          Key k = 0;
-          if (lane == src) {
-            const int e = __ffs(mask) - 1;
-            mask &= mask - 1;
-            k = make_key(E::load(base, i0 + e), i0 + e);
-          }
-          k = __shfl_sync(0xFFFFFFFFu, k, src);
-          if (k > kth) {
-            list = insert(list, k, lane);
-            kth = __shfl_sync(0xFFFFFFFFu, list, p.top - 1);
+            for (int e = 0; e < 8; ++e) {
+              if (x[u][e] >= least && v0 + u * stride < nvec) {
+                const Key k = make_key(x[u][e], (uint32_t)(head + (v0 + u * stride) * 8 + e));
+                if (k >= bound) {
+                  const int at = atomicAdd(&c.count, 1);
+                  if (at < kMostKeys) c.keys[at] = k;
+                  added = true;
+                }
+              }
+            }
           }
         }
-        full = kth != 0;
-        if (full) floor_value = key_value(kth);
+        if (!__syncthreads_or(added)) break;
+        const int n = c.count;
+        __syncthreads();
+        if (n <= kSortAbove) {
+          held = n;
+          break;
+        }
+        sort_out<NT>(c, min(n, kMostKeys), p.top);
+        bound = c.best[p.top - 1];
+        // all of them seen: the best stay. More than there is room for: this round again, from what was there before it, with the higher bound
+        // (at least kMostKeys - 32 elements lie below that, so a round ends)
+        const bool again = n > kMostKeys;
+        if (!again && threadIdx.x < p.top) c.keys[threadIdx.x] = c.best[threadIdx.x];
+        if (!again) held = p.top;
+        if (threadIdx.x == 0) c.count = held;
+        __syncthreads();
+        if (!again) break;
       }
     }
   }
 
+  Stats st = {m, s.x + s.y, t.x + t.y};
   // elements before and behind the vectors: one a lane of the first CTA's last warp
+  if (TOP) __syncthreads();  // (c.count is set)
   if (part == 0 && warp == kWarps - 1) {
     const int i = lane < head ? lane : tail0 + (lane - head);
     const bool live = i < p.classes;
-    const float x = live ? E::load(base, i) : 0.0f;
-    if (live) st = join(st, {fmaxf(x, -INFINITY), x == -INFINITY ? 0.0f : x - x + 1.0f, 0.0f});  // (x - x: NaN for NaN and +infinity)
-    if (TOP) list = merge_lists(list, sort32(live && x == x ? make_key(x, (uint32_t)i) : 0, lane), lane);
+    const float z = live ? E::load(base, i) : 0.0f;
+    if (live) st = join(st, {fmaxf(z, -INFINITY), z == -INFINITY ? 0.0f : z - z + 1.0f, 0.0f});  // (z - z: NaN for NaN and +infinity)
+    // (at most 14 more than kSortAbove)
+    if (TOP && live && z == z && make_key(z, (uint32_t)i) >= bound) c.keys[atomicAdd(&c.count, 1)] = make_key(z, (uint32_t)i);
   }
 
   // lanes, warps, CTAs
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1)
     st = join(st, {__shfl_xor_sync(0xFFFFFFFFu, st.m, d), __shfl_xor_sync(0xFFFFFFFFu, st.s, d), __shfl_xor_sync(0xFFFFFFFFu, st.t, d)});
-  if (lane == 0) stats[warp] = st;
-  if (TOP) lists[warp][lane] = list;
-  __syncthreads();
-  if (TOP) {
+  if constexpr (NT > 32) {
+    if (lane == 0) stats[warp] = st;
+    __syncthreads();
+    if (TOP || warp == 0) {  // (with alternatives every warp needs them)
+      st = stats[lane % kWarps];
 #pragma unroll
-    for (int d = kWarps / 2; d > 0; d >>= 1) {
-      if (warp < d) {
-        list = merge_lists(list, lists[warp + d][lane], lane);
-        lists[warp][lane] = list;
-      }
-      __syncthreads();
+      for (int d = kWarps / 2; d > 0; d >>= 1)
+        st = join(st, {__shfl_xor_sync(0xFFFFFFFFu, st.m, d), __shfl_xor_sync(0xFFFFFFFFu, st.s, d), __shfl_xor_sync(0xFFFFFFFFu, st.t, d)});
     }
+  } else if (TOP) {
+    __syncthreads();
   }
-  if (warp == 0) {
-    st = lane < kWarps ? stats[lane] : Stats{-INFINITY, 0.0f, 0.0f};
-#pragma unroll
-    for (int d = kWarps / 2; d > 0; d >>= 1)
-      st = join(st, {__shfl_xor_sync(0xFFFFFFFFu, st.m, d), __shfl_xor_sync(0xFFFFFFFFu, st.s, d), __shfl_xor_sync(0xFFFFFFFFu, st.t, d)});
-    if (lane == 0) stats[0] = st;
-  }
-  if (parts > 1) {
+  if (TOP) sort_out<NT>(c, c.count, p.top);
+  if (NT > 32 && parts > 1) {
+    if (TOP) __syncthreads();  // all warps have read stats
+    if (threadIdx.x == 0) stats[0] = st;
     ptx::cluster_sync();
     if (part == 0) {
-      if (warp == 0) {
-        st = {-INFINITY, 0.0f, 0.0f};
-        if (lane < (int)parts) {
-          const uint32_t at = ptx::map_to_cta(&stats[0], (uint32_t)lane);
-          st = {ptx::ld_cluster_f32(at), ptx::ld_cluster_f32(at + 4), ptx::ld_cluster_f32(at + 8)};
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
-          st = join(st, {__shfl_xor_sync(0xFFFFFFFFu, st.m, d), __shfl_xor_sync(0xFFFFFFFFu, st.s, d), __shfl_xor_sync(0xFFFFFFFFu, st.t, d)});
+      st = {-INFINITY, 0.0f, 0.0f};
+      if (lane < (int)parts) {
+        const uint32_t at = ptx::map_to_cta(&stats[0], (uint32_t)lane);
+        st = {ptx::ld_cluster_f32(at), ptx::ld_cluster_f32(at + 4), ptx::ld_cluster_f32(at + 8)};
       }
-      if (TOP) {
-        // (a cluster has at most as many CTAs as a CTA has warps)
-        list = warp < (int)parts ? ptx::ld_cluster_u64(ptx::map_to_cta(&lists[0][lane], (uint32_t)warp)) : 0;
-        __syncthreads();  // the first CTA's own list has been read
-        lists[warp][lane] = list;
-        __syncthreads();
 #pragma unroll
-        for (int d = kWarps / 2; d > 0; d >>= 1) {
-          if (warp < d) {
-            list = merge_lists(list, lists[warp + d][lane], lane);
-            lists[warp][lane] = list;
-          }
-          __syncthreads();
-        }
+      for (int d = kMostParts / 2; d > 0; d >>= 1)
+        st = join(st, {__shfl_xor_sync(0xFFFFFFFFu, st.m, d), __shfl_xor_sync(0xFFFFFFFFu, st.s, d), __shfl_xor_sync(0xFFFFFFFFu, st.t, d)});
+      if (TOP) {
+        for (int i = threadIdx.x; i < (int)parts * 32; i += NT)
+          c.keys[i] = (i & 31) < p.top ? ptx::ld_cluster_u64(ptx::map_to_cta(&c.best[i & 31], (uint32_t)i >> 5)) : 0;
+        __syncthreads();
       }
     }
     ptx::cluster_sync();  // the others' shared memory has been read
+    if (part != 0) return;
+    if (TOP) sort_out<NT>(c, (int)parts * 32, p.top);
   }
-  if (part != 0 || warp != 0) return;
   st = {__shfl_sync(0xFFFFFFFFu, st.m, 0), __shfl_sync(0xFFFFFFFFu, st.s, 0), __shfl_sync(0xFFFFFFFFu, st.t, 0)};
+  if (warp != 0) return;
   const bool empty = st.m == -INFINITY && st.s == 0.0f;  // nothing but -infinity
   const float log_s = logf(st.s);
-  const float lse = empty ? -INFINITY : st.m + log_s;
   if (lane == 0) {
-    const int64_t t = p.targets[row];
+    const int64_t target = p.targets[row];
     float lp = 0.0f;
-    if (t >= p.classes) lp = NAN;
-    else if (t >= 0) lp = empty ? -INFINITY : (E::load(base, t) - st.m) - log_s;
+    if (target >= p.classes) lp = NAN;
+    else if (target >= 0) lp = empty ? -INFINITY : (E::load(base, target) - st.m) - log_s;
     p.logprob[row] = lp;
-    if (p.lse) p.lse[row] = lse;
+    if (p.lse) p.lse[row] = empty ? -INFINITY : st.m + log_s;
     if (p.entropy) p.entropy[row] = empty ? 0.0f : log_s - st.t / st.s;
   }
   if (TOP && lane < p.top) {
-    if (p.top_token) p.top_token[row * p.top + lane] = list ? (int64_t)(uint32_t)~(uint32_t)list : -1;
-    if (p.top_logprob) p.top_logprob[row * p.top + lane] = !list ? NAN : empty ? -INFINITY : (key_value(list) - st.m) - log_s;
+    const Key k = c.best[lane];
+    if (p.top_token) p.top_token[row * p.top + lane] = k ? (int64_t)(uint32_t)~(uint32_t)k : -1;
+    if (p.top_logprob) p.top_logprob[row * p.top + lane] = !k ? NAN : empty ? -INFINITY : (key_value(k) - st.m) - log_s;
   }
 }
 
@@ -297,6 +297,7 @@ struct GradParams {
   const float *lse, *entropy, *d_logprob, *d_entropy;  // d_logprob, or d_entropy (then entropy too): optional
   int64_t rows, K, classes;
   uint32_t seed_lo, seed_hi;
+  bool aligned32;  // logits and grad start on 32-byte boundaries
   void* grad;  // optional
   uint4* values;
   uint16_t* meta;
@@ -305,9 +306,10 @@ struct GradParams {
 // What a row's elements have in common: d z = -p (c + h log p), and `hot` at the target's column.
 struct RowTerms {
   float lse, c, h, hot;
-  int64_t target;  // -1: none
+  int64_t target;
   bool empty;
 };
+template <bool ENTROPY>
 __device__ __forceinline__ RowTerms row_terms(const GradParams& p, int64_t row) {
   RowTerms r;
   r.lse = p.lse[row];
@@ -316,117 +318,170 @@ __device__ __forceinline__ RowTerms row_terms(const GradParams& p, int64_t row) 
   float g = p.d_logprob ? p.d_logprob[row] : 0.0f;
   if (r.target < 0) g = 0.0f;
   if (r.target >= p.classes) g = NAN;
-  r.h = p.d_entropy ? p.d_entropy[row] : 0.0f;
-  r.c = p.d_entropy ? fmaf(r.h, p.entropy[row], g) : g;
+  r.h = ENTROPY ? p.d_entropy[row] : 0.0f;
+  r.c = ENTROPY ? fmaf(r.h, p.entropy[row], g) : g;
   r.hot = g;
   return r;
 }
-__device__ __forceinline__ float grad_of(const RowTerms& r, float x) {
-  const float logp = max_nan(x - r.lse, kFarBelow);
-  return -exp2_approx(logp * kLog2e) * fmaf(r.h, logp, r.c);
+template <bool ENTROPY>
+__device__ __forceinline__ float2 grad_of(const RowTerms& r, float2 x) {
+  float2 logp = add2(x, {-r.lse, -r.lse});
+  if (ENTROPY) logp = {max_nan(logp.x, kFarBelow), max_nan(logp.y, kFarBelow)};  // (0 times a number, not 0 times infinity)
+  const float2 d = mul2(logp, {kLog2e, kLog2e}), w = {exp2_approx(d.x), exp2_approx(d.y)};
+  return mul2(w, ENTROPY ? fma2({-r.h, -r.h}, logp, {-r.c, -r.c}) : float2{-r.c, -r.c});
 }
 
-// Two vectors of eight a thread, all rows as one sequence of elements; they end inside a row wherever K is no multiple of 16.
-// N == 0: nothing is pruned.
-template <int DT, int M, int N, int SCHEME>
-__global__ void __launch_bounds__(kThreads)
+constexpr int kGradThreads = 256;
+constexpr int kGradUnits = 2;  // pairs of vectors of a thread
+
+// Sixteen elements, two vectors, in memory order.
+template <int DT>
+__device__ __forceinline__ void load_unit(const void* src, int64_t i, bool aligned32, typename Element<DT>::Raw (&r)[2]) {
+  const uint8_t* q = (const uint8_t*)src + i * Element<DT>::kBytes;
+  auto load32 = [&](const uint8_t* at, uint4& a, uint4& b) {
+    if (aligned32) {
+      asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                   : "l"(at)
+                   : "memory");
+    } else {
+      a = *(const uint4*)at;
+      b = *(const uint4*)(at + 16);
+    }
+  };
+  if constexpr (Element<DT>::k32) {
+    load32(q, r[0].a, r[0].b);
+    load32(q + 32, r[1].a, r[1].b);
+  } else {
+    load32(q, r[0].a, r[1].a);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_unit(void* dst, int64_t i, bool aligned32, const typename Element<DT>::Raw (&r)[2]) {
+  uint8_t* q = (uint8_t*)dst + i * Element<DT>::kBytes;
+  auto store32 = [&](uint8_t* at, const uint4& a, const uint4& b) {
+    if (aligned32) {
+      const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      ptx::st_global_256(at, w);
+    } else {
+      *(uint4*)at = a;
+      *(uint4*)(at + 16) = b;
+    }
+  };
+  if constexpr (Element<DT>::k32) {
+    store32(q, r[0].a, r[0].b);
+    store32(q + 32, r[1].a, r[1].b);
+  } else {
+    store32(q, r[0].a, r[1].a);
+  }
+}
+
+// Units of two vectors, all rows as one sequence of elements; a unit lies inside a row wherever K is a multiple of 16. N == 0: nothing
+// is pruned. ENTROPY: d_entropy is there.
+template <int DT, int M, int N, int SCHEME, bool ENTROPY>
+__global__ void __launch_bounds__(kGradThreads)
 logprob_grad_kernel(const GradParams p) {
   using E = Element<DT>;
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
-  const int64_t total = p.rows * p.K, pair = (int64_t)blockIdx.x * kThreads + threadIdx.x, i0 = pair * 16;
-  const bool on = i0 < total;
-  if (M == 32 ? !__any_sync(0xFFFFFFFFu, on) : !on) return;
-  float x[2][8];
-  typename E::Raw raw[2];
-  if (!on) {
-    raw[0].a = raw[0].b = raw[1].a = raw[1].b = make_uint4(0u, 0u, 0u, 0u);
-  } else {
-    const bool fits32 = total <= 0xFFFFFFFFll;
-    int64_t row = fits32 ? (int64_t)((uint32_t)i0 / (uint32_t)p.K) : i0 / p.K;
-    int64_t col = i0 - row * p.K;
-    RowTerms r = row_terms(p, row);
-    if (col + 16 <= p.K) {
-      raw[0] = E::load8(p.logits, i0);
-      raw[1] = E::load8(p.logits, i0 + 8);
-      const bool whole = col + 16 <= p.classes;
-      const int64_t hot = r.target - col;
+  const int64_t total = p.rows * p.K, unit0 = (int64_t)blockIdx.x * (kGradThreads * kGradUnits) + threadIdx.x;
+  const bool fits32 = total <= 0xFFFFFFFFll;
+  typename E::Raw raw[kGradUnits][2];
+  RowTerms terms[kGradUnits];
+  int64_t col[kGradUnits];
 #pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        E::widen(raw[v], x[v]);
+  for (int u = 0; u < kGradUnits; ++u) {
+    const int64_t i0 = (unit0 + u * kGradThreads) * 16;
+    raw[u][0].a = raw[u][0].b = raw[u][1].a = raw[u][1].b = make_uint4(0u, 0u, 0u, 0u);
+    col[u] = 0;
+    if (i0 < total) {
+      const int64_t row = fits32 ? (int64_t)((uint32_t)i0 / (uint32_t)p.K) : i0 / p.K;
+      col[u] = i0 - row * p.K;
+      if (i0 + 16 <= total) load_unit<DT>(p.logits, i0, p.aligned32, raw[u]);
+      terms[u] = row_terms<ENTROPY>(p, row);
+    }
+  }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[v][e] = grad_of(r, x[v][e]);
+  for (int u = 0; u < kGradUnits; ++u) {
+    const int64_t unit = unit0 + u * kGradThreads, i0 = unit * 16;
+    const bool on = i0 < total;
+    if (M == 32 ? !__any_sync(0xFFFFFFFFu, on) : !on) continue;
+    float x[2][8];
+    E::widen(raw[u][0], x[0]);
+    E::widen(raw[u][1], x[1]);
+    RowTerms& r = terms[u];
+    if (on && col[u] + 16 <= p.K) {
+#pragma unroll
+      for (int k = 0; k < 16; k += 2) {
+        const float2 g = grad_of<ENTROPY>(r, {x[k >> 3][k & 7], x[k >> 3][(k & 7) + 1]});
+        x[k >> 3][k & 7] = g.x;
+        x[k >> 3][(k & 7) + 1] = g.y;
       }
+      const int64_t hot = r.target - col[u];
       if ((uint64_t)hot < 16u && r.target < p.classes) {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
           if (k == hot) x[k >> 3][k & 7] += r.hot;
       }
-      if (!whole || r.empty) {
+      if (col[u] + 16 > p.classes || r.empty) {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
-          if (r.empty || col + k >= p.classes) x[k >> 3][k & 7] = 0.0f;
+          if (r.empty || col[u] + k >= p.classes) x[k >> 3][k & 7] = 0.0f;
       }
-      raw[0] = E::narrow(x[0]);
-      raw[1] = E::narrow(x[1]);
-      if (p.grad) {
-        E::store8(p.grad, i0, raw[0]);
-        E::store8(p.grad, i0 + 8, raw[1]);
-      }
-    } else {  // a row ends here (only where K is no multiple of 16: nothing is pruned there)
+      raw[u][0] = E::narrow(x[0]);
+      raw[u][1] = E::narrow(x[1]);
+      if (p.grad) store_unit<DT>(p.grad, i0, p.aligned32, raw[u]);
+    } else if (on) {  // a row ends here (only where K is no multiple of 16: nothing is pruned there)
       const int left = (int)min((int64_t)16, total - i0);
-      if (left == 16) {
-        raw[0] = E::load8(p.logits, i0);
-        raw[1] = E::load8(p.logits, i0 + 8);
-        E::widen(raw[0], x[0]);
-        E::widen(raw[1], x[1]);
-      } else {
+      if (left < 16) {
 #pragma unroll
         for (int k = 0; k < 16; ++k) x[k >> 3][k & 7] = k < left ? E::load(p.logits, i0 + k) : 0.0f;
       }
+      int64_t row = (i0 - col[u]) / p.K, at = col[u];
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
-        if (col == p.K && k < left) {
-          col = 0;
-          r = row_terms(p, ++row);
+        if (at == p.K && k < left) {
+          at = 0;
+          r = row_terms<ENTROPY>(p, ++row);
         }
         float g = 0.0f;
-        if (col < p.classes && !r.empty) {
-          g = grad_of(r, x[k >> 3][k & 7]);
-          if (col == r.target) g += r.hot;
+        if (at < p.classes && !r.empty) {
+          g = grad_of<ENTROPY>(r, {x[k >> 3][k & 7], 0.0f}).x;
+          if (at == r.target) g += r.hot;
         }
         x[k >> 3][k & 7] = g;
-        ++col;
+        ++at;
       }
+      raw[u][0] = E::narrow(x[0]);
+      raw[u][1] = E::narrow(x[1]);
       if (left == 16) {
-        E::store8(p.grad, i0, E::narrow(x[0]));
-        E::store8(p.grad, i0 + 8, E::narrow(x[1]));
+        store_unit<DT>(p.grad, i0, p.aligned32, raw[u]);
       } else {
 #pragma unroll
         for (int k = 0; k < 16; ++k)
           if (k < left) E::store(p.grad, i0 + k, x[k >> 3][k & 7]);
       }
-      return;
+      continue;
     }
-  }
-  if constexpr (N > 0) {
-    uint4 out;
-    uint32_t pa, pb;
-    KeepFlags ka, kb;
-    compress_pair<M, N, SCHEME, E::kF16>(raw[0].a, raw[1].a, 2 * pair, p.seed_lo, p.seed_hi, M == 32 ? (int)(threadIdx.x & 1) : 0,
-                                         0xFFFFFFFFu, out, pa, pb, ka, kb);
-    if (!on) return;
-    if (p.values) p.values[pair] = out;
-    if (p.meta) p.meta[pair] = (uint16_t)prmt(pa, pb, 0x0073);
+    if constexpr (N > 0) {
+      uint4 out;
+      uint32_t pa, pb;
+      KeepFlags ka, kb;
+      compress_pair<M, N, SCHEME, E::kF16>(raw[u][0].a, raw[u][1].a, 2 * unit, p.seed_lo, p.seed_hi, M == 32 ? (int)(threadIdx.x & 1) : 0,
+                                           0xFFFFFFFFu, out, pa, pb, ka, kb);
+      if (!on) continue;
+      if (p.values) p.values[unit] = out;
+      if (p.meta) p.meta[unit] = (uint16_t)prmt(pa, pb, 0x0073);
+    }
   }
 }
 
 template <typename... Params>
-cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int cluster, cudaStream_t stream, const Params&... args) {
+cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, int cluster, cudaStream_t stream, const Params&... args) {
   if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -435,41 +490,47 @@ cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int cluster, cudaS
   attr[1].val.clusterDim.x = (unsigned)cluster;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+constexpr int kRowThreads = 256;
+constexpr int kWarpRow = 2048;  // tokens up to which a row is one warp's
+
 template <int DT>
 cudaError_t launch_logprob_typed(const LogprobParams& p, int64_t rows, cudaStream_t stream) {
+  if (p.classes <= kWarpRow)
+    return p.top > 0 ? launch(logprob_kernel<DT, true, 32>, rows, 32, 1, stream, p) : launch(logprob_kernel<DT, false, 32>, rows, 32, 1, stream, p);
   // CTAs that share a row: as many as it has work for, while there are too few rows to fill the multiprocessors
   int cluster = 1;
-  while (cluster < kWarps && rows * cluster < 2 * (int64_t)sm_count() && p.classes > cluster * kThreads * 8) cluster *= 2;
-  return p.top > 0 ? launch(logprob_kernel<DT, true>, rows * cluster, cluster, stream, p)
-                   : launch(logprob_kernel<DT, false>, rows * cluster, cluster, stream, p);
+  while (cluster < kMostParts && rows * cluster < 2 * (int64_t)sm_count() && p.classes > cluster * kRowThreads * 8) cluster *= 2;
+  return p.top > 0 ? launch(logprob_kernel<DT, true, kRowThreads>, rows * cluster, kRowThreads, cluster, stream, p)
+                   : launch(logprob_kernel<DT, false, kRowThreads>, rows * cluster, kRowThreads, cluster, stream, p);
+}
+
+template <int DT, int M, int N, int SCHEME>
+cudaError_t launch_grad_form(const GradParams& p, int64_t blocks, cudaStream_t stream) {
+  return p.d_entropy ? launch(logprob_grad_kernel<DT, M, N, SCHEME, true>, blocks, kGradThreads, 1, stream, p)
+                     : launch(logprob_grad_kernel<DT, M, N, SCHEME, false>, blocks, kGradThreads, 1, stream, p);
 }
 
 template <int DT, int M, int N>
 cudaError_t launch_grad_scheme(const GradParams& p, int scheme, int64_t blocks, cudaStream_t stream) {
-  if (scheme == SDGP_RANDOM) return launch(logprob_grad_kernel<DT, M, N, SDGP_RANDOM>, blocks, 1, stream, p);
-  if (scheme == SDGP_MAGNITUDE) return launch(logprob_grad_kernel<DT, M, N, SDGP_MAGNITUDE>, blocks, 1, stream, p);
-  return launch(logprob_grad_kernel<DT, M, N, SDGP_RESCALED_MAGNITUDE>, blocks, 1, stream, p);
+  if (scheme == SDGP_RANDOM) return launch_grad_form<DT, M, N, SDGP_RANDOM>(p, blocks, stream);
+  if (scheme == SDGP_MAGNITUDE) return launch_grad_form<DT, M, N, SDGP_MAGNITUDE>(p, blocks, stream);
+  return launch_grad_form<DT, M, N, SDGP_RESCALED_MAGNITUDE>(p, blocks, stream);
 }
 
 template <int DT>
 cudaError_t launch_grad_typed(const GradParams& p, int n, int m, int scheme, cudaStream_t stream) {
-  const int64_t blocks = (p.rows * p.K + 16 * kThreads - 1) / (16 * kThreads);
-  if (!p.values && !p.meta) return launch(logprob_grad_kernel<DT, 4, 0, 0>, blocks, 1, stream, p);
+  constexpr int64_t per_block = 16 * kGradThreads * kGradUnits;
+  const int64_t blocks = (p.rows * p.K + per_block - 1) / per_block;
+  if (!p.values && !p.meta) return launch_grad_form<DT, 4, 0, 0>(p, blocks, stream);
   if constexpr (DT != SDGP_FP32) {
-    switch (m * 4 + n) {
-      case 17: return launch_grad_scheme<DT, 4, 1>(p, scheme, blocks, stream);
-      case 18: return launch_grad_scheme<DT, 4, 2>(p, scheme, blocks, stream);
-      case 33: return launch_grad_scheme<DT, 8, 1>(p, scheme, blocks, stream);
-      case 34: return launch_grad_scheme<DT, 8, 2>(p, scheme, blocks, stream);
-      case 65: return launch_grad_scheme<DT, 16, 1>(p, scheme, blocks, stream);
-      case 66: return launch_grad_scheme<DT, 16, 2>(p, scheme, blocks, stream);
-      case 129: return launch_grad_scheme<DT, 32, 1>(p, scheme, blocks, stream);
-      case 130: return launch_grad_scheme<DT, 32, 2>(p, scheme, blocks, stream);
-    }
+#define SDGP_FORM(M, N) \
+  if (m == M && n == N) return launch_grad_scheme<DT, M, N>(p, scheme, blocks, stream);
+    SDGP_FORM(4, 1) SDGP_FORM(4, 2) SDGP_FORM(8, 1) SDGP_FORM(8, 2) SDGP_FORM(16, 1) SDGP_FORM(16, 2) SDGP_FORM(32, 1) SDGP_FORM(32, 2)
+#undef SDGP_FORM
   }
   return cudaErrorInvalidValue;
 }
@@ -490,7 +551,7 @@ cudaError_t launch_token_logprob_backward(const void* logits, const int64_t* tar
                                           int m, int scheme, uint64_t seed, int dtype, void* grad, void* values, void* meta,
                                           cudaStream_t stream) {
   const GradParams p = {logits, targets, lse, entropy, d_logprob, d_entropy, rows, K, classes, (uint32_t)seed, (uint32_t)(seed >> 32),
-                        grad, (uint4*)values, (uint16_t*)meta};
+                        (((uintptr_t)logits | (uintptr_t)grad) & 31u) == 0, grad, (uint4*)values, (uint16_t*)meta};
   if (dtype == SDGP_BF16) return launch_grad_typed<SDGP_BF16>(p, n, m, scheme, stream);
   if (dtype == SDGP_FP16) return launch_grad_typed<SDGP_FP16>(p, n, m, scheme, stream);
   return launch_grad_typed<SDGP_FP32>(p, n, m, scheme, stream);

@@ -41,7 +41,9 @@ struct Ring {
   static constexpr int kChunk = kCtaThreads<TPR> * 16;               // 16 bytes of each thread side by side
   static constexpr int kVec = kChunk * (Element<DT>::kBytes / 2);    // a vector: one chunk, or two of fp32
   static constexpr int kStage = A * kVec;
-  static constexpr int kStages = kStage * 3 <= 100 * 1024 ? 3 : kStage * 2 <= 200 * 1024 ? 2 : 1;
+  // forward: up to 100 KB of two CTAs a multiprocessor; backward: four stages where they fit
+  static constexpr int kStages = A == 2 ? (kStage * 3 <= 100 * 1024 ? 3 : kStage * 2 <= 200 * 1024 ? 2 : 1)
+                                        : (kStage * 4 <= 128 * 1024 ? 4 : kStage * 3 <= 200 * 1024 ? 3 : kStage * 2 <= 200 * 1024 ? 2 : 1);
   static constexpr int kBytes = kStage * kStages;
 };
 
@@ -115,24 +117,37 @@ __device__ __forceinline__ void write_sums(float* dst, const Part& p, const floa
   }
 }
 
-// Sums over the TPR threads of a row. `turn` alternates between two buffers, so one barrier a call is enough.
+// Sums over the TPR threads of a row, in two halves with a barrier of those threads between them (rows of one warp need none).
 template <int TPR, int N>
-__device__ __forceinline__ void row_sums(float (&s)[N], float* buffer, int slot, int& turn) {
+__device__ __forceinline__ void put_sums(float (&s)[N], float* b) {
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i] = warp_sum(s[i]);
+  if (TPR > 32 && (threadIdx.x & 31) == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) b[i * (TPR / 32) + ((threadIdx.x % TPR) >> 5)] = s[i];
+  }
+}
+template <int TPR, int N>
+__device__ __forceinline__ void get_sums(float (&s)[N], const float* b) {
   if constexpr (TPR > 32) {
     constexpr int W = TPR / 32;
-    const int lane = threadIdx.x & 31, warp = (threadIdx.x % TPR) >> 5;
-    float* b = buffer + (turn * (kCtaThreads<TPR> / TPR) + slot) * W * N;
-    if (lane == 0) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-      for (int i = 0; i < N; ++i) b[i * W + warp] = s[i];
+    for (int i = 0; i < N; ++i) {
+      s[i] = b[i * W + lane % W];
+#pragma unroll
+      for (int d = W / 2; d > 0; d >>= 1) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], d);
     }
-    ptx::named_bar_sync(1 + slot, TPR);
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] = warp_sum(lane < W ? b[i * W + lane] : 0.0f);
-    turn ^= 1;
   }
+}
+// At once. `turn` alternates between two buffers, so one barrier a call is enough.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float* buffer, int slot, int& turn) {
+  float* b = buffer + (turn * (kCtaThreads<TPR> / TPR) + slot) * (TPR / 32) * N;
+  put_sums<TPR>(s, b);
+  if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
+  get_sums<TPR>(s, b);
+  turn ^= 1;
 }
 
 // ------------------------------------------------------------------------------------------------ forward
@@ -254,179 +269,247 @@ __device__ __noinline__ uint4 prune_any(uint4 w, int64_t v, uint32_t seed_lo, ui
 }
 
 // Rows are dealt out in units: rows of one gate, at a stride of `splits`. A slot takes units at the stride of all slots.
+struct Walk {
+  int unit, in_group, group;
+  int64_t row;
+};
+__device__ __forceinline__ void settle(Walk& w, const NormGradParams& p, int ids) {  // to the first row at or behind w
+  while (w.unit < p.units && w.in_group >= p.rows_per_group) {
+    w.unit += ids;
+    w.group = w.unit / p.splits;
+    w.in_group = w.unit - w.group * p.splits;
+    w.row = (int64_t)w.group * p.rows_per_group + w.in_group;
+  }
+}
+__device__ __forceinline__ void advance(Walk& w, const NormGradParams& p, int ids) {
+  if (w.unit >= p.units) return;
+  w.in_group += p.splits;
+  w.row += p.splits;
+  settle(w, p, ids);
+}
+
+__device__ __forceinline__ float2 pair_of(const float (&x)[8], int i) { return {x[2 * i], x[2 * i + 1]}; }
+__device__ __forceinline__ float2 both(float x) { return {x, x}; }
+
+// The two means of the formulas hang on each other: mean(q d v) needs d, which needs mean(w_pre d_y u). Written out,
+//   sum q d v = sum q v (d_o + rstd w_pre d_y) - rstd mean(w_pre d_y u) sum q v u,
+// so one exchange of three sums does. They are taken a row ahead: between two barriers a group of threads sums its next row and writes the
+// outputs of the present one, reading its inputs from shared memory a second time instead of keeping them. (With the sums of a row, a
+// barrier and its outputs in turn: 279 us for 16384 x 4096 bf16.)
 template <int DT, int TPR, bool PRUNE>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 256 ? 1 : 2)
 norm_grad_kernel(const NormGradParams p) {
   using E = Element<DT>;
   using R = Ring<DT, TPR, 4>;
-  constexpr int SLOTS = kCtaThreads<TPR> / TPR;
+  constexpr int SLOTS = kCtaThreads<TPR> / TPR, S = R::kStages;
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float buffer[2 * 3 * SLOTS * kMaxWarpsPerRow];
+  __shared__ float buffer[2 * 3 * SLOTS * (TPR / 32)];
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
   const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
   const int id = (int)blockIdx.x * SLOTS + slot, ids = (int)gridDim.x * SLOTS;
-  // rows of the walk: unit u = group * splits + s holds rows group * rows_per_group + s + i * splits
-  struct Walk {
-    int unit;
-    int64_t in_group;
-  };
-  auto row_of = [&](const Walk& w) { return (int64_t)(w.unit / p.splits) * p.rows_per_group + w.in_group; };
-  auto settle = [&](Walk& w) {  // to the first row at or behind w
-    while (w.unit < p.units && w.in_group >= p.rows_per_group) {
-      w.unit += ids;
-      w.in_group = w.unit % p.splits;
-    }
-  };
-  auto advance = [&](Walk& w) {
-    w.in_group += p.splits;
-    settle(w);
-  };
-  Walk here = {id, id % p.splits};
-  settle(here);
+  Walk here;
+  here.unit = id;
+  here.group = id / p.splits;
+  here.in_group = id - here.group * p.splits;
+  here.row = (int64_t)here.group * p.rows_per_group + here.in_group;
+  settle(here, p, ids);
   if (here.unit >= p.units) {
     // no row at all: the sums of this slot are zero
     const Part none = part_of(0, p.C, t);
     const float zero[8] = {};
     if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, none, zero);
     if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, none, zero);
-  } else {
-    const Part part = part_of(row_of(here), p.C, t);
-    uint8_t* mine = ring + threadIdx.x * 16;
-    const uint32_t mine_u32 = ptx::smem_u32(mine);
-    auto fetch = [&](const Walk& w, int stage) {
-      if (w.unit < p.units) {
-        const int64_t row = row_of(w);
-        const uint32_t at = mine_u32 + stage * R::kStage;
-        copy_part<DT, R::kChunk>(at, p.branch, row, p.C, part);
-        if (p.d_out) copy_part<DT, R::kChunk>(at + R::kVec, p.d_out, row, p.C, part);
-        if (p.d_y) {
-          copy_part<DT, R::kChunk>(at + 2 * R::kVec, p.out, row, p.C, part);
-          copy_part<DT, R::kChunk>(at + 3 * R::kVec, p.d_y, row, p.C, part);
-        }
-      }
-      cp_async_commit();
-    };
-    Walk ahead = here;
-#pragma unroll
-    for (int s = 0; s < R::kStages; ++s) {
-      fetch(ahead, s);
-      if (ahead.unit < p.units) advance(ahead);
-    }
-    const typename E::Raw w_post = column_part<DT>(p.post_weight, 0, part), w_pre = column_part<DT>(p.pre_weight, 0, part);
-    typename E::Raw gate = column_part<DT>(p.gate, 0, part);
-    int gate_group = 0;
-    const float inv_c = 1.0f / (float)p.C;
-    float pre_sum[8] = {}, post_sum[8] = {}, gate_sum[8] = {};
-    int stage = 0, turn = 0;
-    while (here.unit < p.units) {
-      const int64_t row = row_of(here);
-      const int group = here.unit / p.splits;
-      if (p.gate && group != gate_group) {
-        gate = column_part<DT>(p.gate, (int64_t)group * p.C, part);
-        gate_group = group;
-      }
-      cp_async_wait<R::kStages - 1>();
-      const uint8_t* at = mine + stage * R::kStage;
-      float v[8], d[8], u[8], q[8], w[8];
-      read_part<DT, R::kChunk>(at, part, v);
-      if (p.d_out) {
-        read_part<DT, R::kChunk>(at + R::kVec, part, d);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = 0.0f;
-      }
-      if (p.post_weight) {
-        const float rstd = p.post_rstd[row];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= rstd;
-      }
-      // q = g w_post, the factor from d to the normalised branch's gradient
-      E::widen(gate, q);
-      E::widen(w_post, w);
-      if (p.post_weight) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) q[e] *= w[e];
-      }
-      // The two means of the formulas hang on each other: mean(q d v) needs d, which needs mean(w_pre d_y u). Written out,
-      //   sum q d v = sum q v (d_o + rstd w_pre d_y) - rstd mean(w_pre d_y u) sum q v u,
-      // so one exchange of three sums does.
-      float s[3] = {0.0f, 0.0f, 0.0f};
-      float rstd = 0.0f;
-      if (p.d_y) {
-        rstd = p.pre_rstd[row];
-        float dy[8];
-        read_part<DT, R::kChunk>(at + 2 * R::kVec, part, u);
-        read_part<DT, R::kChunk>(at + 3 * R::kVec, part, dy);
-        E::widen(w_pre, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          u[e] *= rstd;
-          pre_sum[e] = fmaf(dy[e], u[e], pre_sum[e]);
-          const float wd = dy[e] * w[e];
-          s[0] = fmaf(wd, u[e], s[0]);
-          d[e] = fmaf(rstd, wd, d[e]);
-          s[2] = fmaf(q[e] * v[e], u[e], s[2]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = 0.0f;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[1] = fmaf(q[e] * v[e], d[e], s[1]);
-      if (p.d_y || p.post_weight) row_sums<TPR>(s, buffer, slot, turn);
-      const float k = rstd * (s[0] * inv_c);
-      const float mean = (s[1] - k * s[2]) * inv_c;
-      float out[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        d[e] = fmaf(-k, u[e], d[e]);
-        out[e] = p.alpha * d[e];
-      }
-      if (p.d_residual) write_part<DT>(p.d_residual, row, p.C, part, E::narrow(out), out);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) gate_sum[e] = fmaf(d[e], v[e], gate_sum[e]);
-      if (p.post_weight) {
-        const float rstd_b = p.post_rstd[row];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = rstd_b * fmaf(q[e], d[e], -v[e] * mean);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = q[e] * d[e];
-      }
-      const typename E::Raw packed = E::narrow(out);
-      if (p.d_branch) write_part<DT>(p.d_branch, row, p.C, part, packed, out);
-      if constexpr (PRUNE) {  // (rows of whole groups of 16: every part is full or empty, and a group's lanes alike)
-        const int64_t vec = row * (p.C / 8) + t;
-        const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, t & 3);
-        if (part.full) {
-          if (p.values) p.values[vec] = make_uint2(c.x, c.y);
-          if (p.meta) p.meta[vec] = (uint8_t)c.z;
-        }
-      }
-      const Walk last = here;
-      advance(here);
-      if (here.unit != last.unit) {  // the unit's rows are done: sum of d v over them
-        E::widen(gate, q);
-        E::widen(w_post, w);
-        float g[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          post_sum[e] = fmaf(q[e], gate_sum[e], post_sum[e]);
-          g[e] = p.post_weight ? w[e] * gate_sum[e] : gate_sum[e];
-          gate_sum[e] = 0.0f;
-        }
-        if (p.gate_sums) write_sums(p.gate_sums + ((int64_t)group * p.gate_rows + last.unit % p.splits) * p.C, part, g);
-        else if (p.d_gate) write_sums(p.d_gate + (int64_t)group * p.C, part, g);
-      }
-      fetch(ahead, stage);
-      if (ahead.unit < p.units) advance(ahead);
-      if (++stage == R::kStages) stage = 0;
-    }
-    cp_async_wait<0>();
-    if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, part, pre_sum);
-    if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, part, post_sum);
+    return;
   }
+  const Part part = part_of(here.row, p.C, t);
+  uint8_t* mine = ring + threadIdx.x * 16;
+  const uint32_t mine_u32 = ptx::smem_u32(mine);
+  auto fetch = [&](const Walk& w, int stage) {
+    if (w.unit < p.units) {
+      const uint32_t at = mine_u32 + stage * R::kStage;
+      copy_part<DT, R::kChunk>(at, p.branch, w.row, p.C, part);
+      if (p.d_out) copy_part<DT, R::kChunk>(at + R::kVec, p.d_out, w.row, p.C, part);
+      if (p.d_y) {
+        copy_part<DT, R::kChunk>(at + 2 * R::kVec, p.out, w.row, p.C, part);
+        copy_part<DT, R::kChunk>(at + 3 * R::kVec, p.d_y, w.row, p.C, part);
+      }
+    }
+    cp_async_commit();
+  };
+  // what belongs to a row beside its elements, loaded a row before it is summed
+  struct Beside {
+    float rstd_b, rstd;
+    typename E::Raw gate;
+  };
+  auto load_beside = [&](const Walk& w, int known_group, Beside& b) {
+    if (w.unit >= p.units) return;
+    b.rstd_b = p.post_weight ? p.post_rstd[w.row] : 1.0f;
+    b.rstd = p.d_y ? p.pre_rstd[w.row] : 0.0f;
+    if (w.group != known_group) b.gate = column_part<DT>(p.gate, p.gate ? (int64_t)w.group * p.C : 0, part);
+  };
+  const typename E::Raw w_post = column_part<DT>(p.post_weight, 0, part), w_pre = column_part<DT>(p.pre_weight, 0, part);
+  auto factors = [&](const Beside& beside, float (&q)[8]) {  // q = g w_post
+    float w[8];
+    E::widen(beside.gate, q);
+    E::widen(w_post, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] *= w[e];
+  };
+  const float inv_c = 1.0f / (float)p.C;
+  auto sum_row = [&](const Beside& beside, int stage, int turn) {
+    const uint8_t* at = mine + stage * R::kStage;
+    float b[8], q[8], d[8];
+    read_part<DT, R::kChunk>(at, part, b);
+    factors(beside, q);
+    float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
+    if (p.d_out) {
+      read_part<DT, R::kChunk>(at + R::kVec, part, d);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = 0.0f;
+    }
+    if (p.d_y) {
+      float o[8], y[8], w[8];
+      read_part<DT, R::kChunk>(at + 2 * R::kVec, part, o);
+      read_part<DT, R::kChunk>(at + 3 * R::kVec, part, y);
+      E::widen(w_pre, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 wd = mul2(pair_of(y, i), pair_of(w, i)), qb = mul2(pair_of(q, i), pair_of(b, i));
+        s0 = fma2(wd, pair_of(o, i), s0);
+        s1 = fma2(qb, fma2(both(beside.rstd), wd, pair_of(d, i)), s1);
+        s2 = fma2(qb, pair_of(o, i), s2);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s1 = fma2(mul2(pair_of(q, i), pair_of(b, i)), pair_of(d, i), s1);
+    }
+    float s[3] = {beside.rstd * (s0.x + s0.y), beside.rstd_b * (s1.x + s1.y), beside.rstd_b * beside.rstd * (s2.x + s2.y)};
+    float* to = buffer + (turn * SLOTS + slot) * (TPR / 32) * 3;
+    put_sums<TPR>(s, to);
+    return make_float3(s[0], s[1], s[2]);  // (rows of one warp: these are the sums)
+  };
+
+  Walk next = here;
+  advance(next, p, ids);
+  Walk after = next, ahead = here;
+  advance(after, p, ids);
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    fetch(ahead, s);
+    advance(ahead, p, ids);
+  }
+  Beside beside = {}, beside_next = {}, beside_after = {};
+  load_beside(here, -1, beside);
+  beside_next = beside;
+  load_beside(next, here.group, beside_next);
+  beside_after = beside_next;
+  cp_async_wait<S - 1>();
+  float3 own = sum_row(beside, 0, 0), own_next = own;
+  if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
+
+  float2 pre_sum[4] = {}, post_sum[4] = {}, gate_sum[4] = {};
+  int stage = 0, turn = 0;
+  while (here.unit < p.units) {
+    const int stage_next = stage + 1 == S ? 0 : stage + 1;
+    load_beside(after, next.group, beside_after);
+    if (next.unit < p.units) {
+      cp_async_wait<(S > 1 ? S - 2 : 0)>();
+      own_next = sum_row(beside_next, stage_next, turn ^ 1);
+    }
+    float s[3] = {own.x, own.y, own.z};
+    get_sums<TPR>(s, buffer + (turn * SLOTS + slot) * (TPR / 32) * 3);
+    const float k = beside.rstd * (s[0] * inv_c), mean = (s[1] - k * s[2]) * inv_c;
+    const uint8_t* at = mine + stage * R::kStage;
+    float b[8], q[8], d[8];
+    read_part<DT, R::kChunk>(at, part, b);
+    if (p.d_out) {
+      read_part<DT, R::kChunk>(at + R::kVec, part, d);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = 0.0f;
+    }
+    if (p.d_y) {
+      float o[8], y[8], w[8];
+      read_part<DT, R::kChunk>(at + 2 * R::kVec, part, o);
+      read_part<DT, R::kChunk>(at + 3 * R::kVec, part, y);
+      E::widen(w_pre, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 dy = pair_of(y, i), u = mul2(pair_of(o, i), both(beside.rstd));
+        pre_sum[i] = fma2(dy, u, pre_sum[i]);
+        const float2 x = fma2(both(-k), u, fma2(both(beside.rstd), mul2(dy, pair_of(w, i)), pair_of(d, i)));
+        d[2 * i] = x.x;
+        d[2 * i + 1] = x.y;
+      }
+    }
+    float out[8];
+    if (p.d_residual) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) out[e] = p.alpha * d[e];
+      write_part<DT>(p.d_residual, here.row, p.C, part, E::narrow(out), out);
+    }
+    factors(beside, q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = pair_of(d, i), v = mul2(pair_of(b, i), both(beside.rstd_b));
+      gate_sum[i] = fma2(x, v, gate_sum[i]);
+      float2 y = mul2(pair_of(q, i), x);
+      if (p.post_weight) y = mul2(fma2(v, both(-mean), y), both(beside.rstd_b));
+      out[2 * i] = y.x;
+      out[2 * i + 1] = y.y;
+    }
+    const typename E::Raw packed = E::narrow(out);
+    if (p.d_branch) write_part<DT>(p.d_branch, here.row, p.C, part, packed, out);
+    if constexpr (PRUNE) {  // (rows of whole groups of 16: every part is full or empty, and a group's lanes alike)
+      const int64_t vec = here.row * (p.C / 8) + t;
+      const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, t & 3);
+      if (part.full) {
+        if (p.values) p.values[vec] = make_uint2(c.x, c.y);
+        if (p.meta) p.meta[vec] = (uint8_t)c.z;
+      }
+    }
+    if (here.unit != next.unit) {  // the unit's rows are done: sum of d v over them
+      float g[8], w[8];
+      E::widen(beside.gate, g);
+      E::widen(w_post, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        post_sum[i] = fma2(pair_of(g, i), gate_sum[i], post_sum[i]);
+        out[2 * i] = w[2 * i] * gate_sum[i].x;
+        out[2 * i + 1] = w[2 * i + 1] * gate_sum[i].y;
+        gate_sum[i] = both(0.0f);
+      }
+      if (p.gate_sums) write_sums(p.gate_sums + ((int64_t)here.group * p.gate_rows + (here.unit - here.group * p.splits)) * p.C, part, out);
+      else if (p.d_gate) write_sums(p.d_gate + (int64_t)here.group * p.C, part, out);
+    }
+    fetch(ahead, stage);
+    advance(ahead, p, ids);
+    here = next;
+    next = after;
+    advance(after, p, ids);
+    beside = beside_next;
+    beside_next = beside_after;
+    own = own_next;
+    stage = stage_next;
+    turn ^= 1;
+    if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
+  }
+  cp_async_wait<0>();
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = pre_sum[i].x;
+    x[2 * i + 1] = pre_sum[i].y;
+  }
+  if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, part, x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = post_sum[i].x;
+    x[2 * i + 1] = post_sum[i].y;
+  }
+  if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, part, x);
 }
 
 // Sums of the slots' sums, in a fixed order. Job 0: d_pre_weight, 1: d_post_weight, 2 + g: gate g.
@@ -750,7 +833,8 @@ cudaError_t launch_forward(const NormParams& p, const Plan& plan, cudaStream_t s
 
 template <int DT, bool PRUNE>
 cudaError_t launch_backward(const NormGradParams& p, const Plan& plan, cudaStream_t stream) {
-  switch (plan.tpr) {
+  // (fp32 rows of 1024 threads leave room for one stage only, and a row ahead needs two)
+  switch (DT == SDGP_FP32 && plan.tpr == 1024 ? 0 : plan.tpr) {
 #define SDGP_ROW(T) \
   case T: return launch<norm_grad_kernel<DT, T, PRUNE>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 4>::kBytes, stream, p);
     SDGP_ROW(32) SDGP_ROW(64) SDGP_ROW(128) SDGP_ROW(256) SDGP_ROW(512) SDGP_ROW(1024)

@@ -36,14 +36,14 @@ __device__ __forceinline__ void cp_async_wait() {
 // Threads of a CTA, and stages of the copies that are under way, for rows of TPR threads and A input tensors.
 template <int TPR>
 constexpr int kCtaThreads = TPR > 256 ? TPR : 256;
-template <int DT, int TPR, int A>
-struct Ring {
+template <int DT, int TPR, int VECTORS, int LEAST>
+struct Ring {  // VECTORS: of a thread and row, in all tensors; LEAST: stages that a kernel cannot do without
   static constexpr int kChunk = kCtaThreads<TPR> * 16;               // 16 bytes of each thread side by side
   static constexpr int kVec = kChunk * (Element<DT>::kBytes / 2);    // a vector: one chunk, or two of fp32
-  static constexpr int kStage = A * kVec;
-  // forward: up to 100 KB of two CTAs a multiprocessor; backward: four stages where they fit
-  static constexpr int kStages = A == 2 ? (kStage * 3 <= 100 * 1024 ? 3 : kStage * 2 <= 200 * 1024 ? 2 : 1)
-                                        : (kStage * 4 <= 128 * 1024 ? 4 : kStage * 3 <= 200 * 1024 ? 3 : kStage * 2 <= 200 * 1024 ? 2 : 1);
+  static constexpr int kStage = VECTORS * kVec;
+  static constexpr int kRoom = (TPR > 256 ? 200 : 100) * 1024;       // (CTAs of 256 threads share a multiprocessor)
+  static constexpr int kFit = kRoom / kStage;
+  static constexpr int kStages = kFit > 4 ? 4 : kFit < LEAST ? LEAST : kFit;
   static constexpr int kBytes = kStage * kStages;
 };
 
@@ -64,33 +64,33 @@ __device__ __forceinline__ Part part_of(int64_t row, int C, int t) {
 }
 
 template <int DT, int CHUNK>
-__device__ __forceinline__ void copy_part(uint32_t dst, const void* src, int64_t row, int C, const Part& p) {
+__device__ __forceinline__ void copy_part(uint32_t dst, const void* src, int64_t row_at, const Part& p) {
   using E = Element<DT>;
-  const uint8_t* q = (const uint8_t*)src + (row * C + p.first) * E::kBytes;
+  const uint8_t* q = (const uint8_t*)src + (row_at + p.first) * E::kBytes;
   const int bytes = p.hi * E::kBytes;
   cp_async16(dst, q, (uint32_t)min(16, bytes));
   if (E::k32) cp_async16(dst + CHUNK, bytes > 16 ? q + 16 : q, (uint32_t)max(0, bytes - 16));
 }
-template <int DT, int CHUNK>
+template <int DT, int CHUNK, bool ALIGNED>
 __device__ __forceinline__ void read_part(const uint8_t* at, const Part& p, float (&x)[8]) {
   using E = Element<DT>;
   typename E::Raw r;
   r.a = *(const uint4*)at;
   r.b = E::k32 ? *(const uint4*)(at + CHUNK) : make_uint4(0u, 0u, 0u, 0u);
   E::widen(r, x);
-  if (!p.full) {
+  if (!ALIGNED && p.lo != 0) {  // the end of the row before (what lies behind the row was never copied and is zero)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (e < p.lo || e >= p.hi) x[e] = 0.0f;
+      if (e < p.lo) x[e] = 0.0f;
   }
 }
-template <int DT>
-__device__ __forceinline__ void write_part(void* dst, int64_t row, int C, const Part& p, const typename Element<DT>::Raw& r, const float (&x)[8]) {
+template <int DT, bool ALIGNED = false>
+__device__ __forceinline__ void write_part(void* dst, int64_t row_at, const Part& p, const typename Element<DT>::Raw& r, const float (&x)[8]) {
   using E = Element<DT>;
-  const int64_t at = row * C + p.first;
+  const int64_t at = row_at + p.first;
   if (p.full) {
     E::store8(dst, at, r);
-  } else {
+  } else if (!ALIGNED) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e >= p.lo && e < p.hi) E::store(dst, at + e, x[e]);
@@ -118,36 +118,33 @@ __device__ __forceinline__ void write_sums(float* dst, const Part& p, const floa
 }
 
 // Sums over the TPR threads of a row, in two halves with a barrier of those threads between them (rows of one warp need none).
-template <int TPR, int N>
-__device__ __forceinline__ void put_sums(float (&s)[N], float* b) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) s[i] = warp_sum(s[i]);
-  if (TPR > 32 && (threadIdx.x & 31) == 0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) b[i * (TPR / 32) + ((threadIdx.x % TPR) >> 5)] = s[i];
-  }
+template <int TPR>
+__device__ __forceinline__ void put_sum(float s, float* b) {
+  s = warp_sum(s);
+  if ((threadIdx.x & 31) == 0) b[(threadIdx.x % TPR) >> 5] = s;
 }
-template <int TPR, int N>
-__device__ __forceinline__ void get_sums(float (&s)[N], const float* b) {
-  if constexpr (TPR > 32) {
-    constexpr int W = TPR / 32;
-    const int lane = threadIdx.x & 31;
+template <int W>
+__device__ __forceinline__ float sum_lanes(float s) {  // over W neighbouring lanes
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      s[i] = b[i * W + lane % W];
-#pragma unroll
-      for (int d = W / 2; d > 0; d >>= 1) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], d);
-    }
-  }
+  for (int d = W / 2; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  return s;
 }
 // At once. `turn` alternates between two buffers, so one barrier a call is enough.
 template <int TPR, int N>
 __device__ __forceinline__ void row_sums(float (&s)[N], float* buffer, int slot, int& turn) {
-  float* b = buffer + (turn * (kCtaThreads<TPR> / TPR) + slot) * (TPR / 32) * N;
-  put_sums<TPR>(s, b);
-  if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
-  get_sums<TPR>(s, b);
-  turn ^= 1;
+  if constexpr (TPR == 32) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = warp_sum(s[i]);
+  } else {
+    constexpr int W = TPR / 32;
+    float* b = buffer + (turn * (kCtaThreads<TPR> / TPR) + slot) * W * N;
+#pragma unroll
+    for (int i = 0; i < N; ++i) put_sum<TPR>(s[i], b + i * W);
+    ptx::named_bar_sync(1 + slot, TPR);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = sum_lanes<W>(b[i * W + (threadIdx.x & 31) % W]);
+    turn ^= 1;
+  }
 }
 
 // ------------------------------------------------------------------------------------------------ forward
@@ -166,7 +163,7 @@ template <int DT, int TPR>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 512 ? 1 : 1024 / kCtaThreads<TPR>)
 norm_kernel(const NormParams p) {
   using E = Element<DT>;
-  using R = Ring<DT, TPR, 2>;
+  using R = Ring<DT, TPR, 2, 1>;
   constexpr int SLOTS = kCtaThreads<TPR> / TPR;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float buffer[2 * SLOTS * kMaxWarpsPerRow];
@@ -180,8 +177,8 @@ norm_kernel(const NormParams p) {
   const uint32_t mine_u32 = ptx::smem_u32(mine);
   auto fetch = [&](int64_t row, int stage) {
     if (row < p.rows) {
-      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage, p.branch, row, p.C, part);
-      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + R::kVec, p.residual, row, p.C, part);
+      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage, p.branch, row * p.C, part);
+      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + R::kVec, p.residual, row * p.C, part);
     }
     cp_async_commit();
   };
@@ -195,8 +192,8 @@ norm_kernel(const NormParams p) {
     if (p.groups > 1) gate = column_part<DT>(p.gate, row / p.rows_per_group * p.C, part);
     cp_async_wait<R::kStages - 1>();
     float b[8], r[8], w[8], g[8];
-    read_part<DT, R::kChunk>(mine + stage * R::kStage, part, b);
-    read_part<DT, R::kChunk>(mine + stage * R::kStage + R::kVec, part, r);
+    read_part<DT, R::kChunk, false>(mine + stage * R::kStage, part, b);
+    read_part<DT, R::kChunk, false>(mine + stage * R::kStage + R::kVec, part, r);
     E::widen(gate, g);
     if (p.post_weight) {
       float s[1] = {0.0f};
@@ -211,7 +208,7 @@ norm_kernel(const NormParams p) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) r[e] = fmaf(g[e], b[e], p.alpha * r[e]);
-    write_part<DT>(p.out, row, p.C, part, E::narrow(r), r);
+    write_part<DT>(p.out, row * p.C, part, E::narrow(r), r);
     if (p.pre_weight) {  // (of the sums before their rounding to 16 bits)
       float s[1] = {0.0f};
 #pragma unroll
@@ -222,7 +219,7 @@ norm_kernel(const NormParams p) {
       E::widen(w_pre, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) r[e] = r[e] * rstd * w[e];
-      write_part<DT>(p.y, row, p.C, part, E::narrow(r), r);
+      write_part<DT>(p.y, row * p.C, part, E::narrow(r), r);
     }
     fetch(row + R::kStages * stride, stage);
     if (++stage == R::kStages) stage = 0;
@@ -268,71 +265,103 @@ __device__ __noinline__ uint4 prune_any(uint4 w, int64_t v, uint32_t seed_lo, ui
   return make_uint4(out.x, out.y, pos >> 24, 0u);
 }
 
-// Rows are dealt out in units: rows of one gate, at a stride of `splits`. A slot takes units at the stride of all slots.
+// Rows are dealt out in units: rows of one gate, at a stride of `splits`. A slot takes units at the stride of all slots (without GATES: one
+// unit).
 struct Walk {
-  int unit, in_group, group;
-  int64_t row;
+  int64_t row, at;  // at = row * C
+  int left;         // rows of the unit from this one on; 0: no row
+  int unit, group;
 };
-__device__ __forceinline__ void settle(Walk& w, const NormGradParams& p, int ids) {  // to the first row at or behind w
-  while (w.unit < p.units && w.in_group >= p.rows_per_group) {
-    w.unit += ids;
+template <bool GATES>
+__device__ __forceinline__ void start_unit(Walk& w, const NormGradParams& p, int ids) {  // the first row of w.unit, or of the next unit that has one
+  w.left = 0;
+  for (; w.unit < p.units; w.unit += ids) {
     w.group = w.unit / p.splits;
-    w.in_group = w.unit - w.group * p.splits;
-    w.row = (int64_t)w.group * p.rows_per_group + w.in_group;
+    const int first = w.unit - w.group * p.splits;
+    w.left = (int)((p.rows_per_group - first + p.splits - 1) / p.splits);
+    w.row = (int64_t)w.group * p.rows_per_group + first;
+    w.at = w.row * p.C;
+    if (w.left > 0 || !GATES) return;
   }
 }
-__device__ __forceinline__ void advance(Walk& w, const NormGradParams& p, int ids) {
-  if (w.unit >= p.units) return;
-  w.in_group += p.splits;
+template <bool GATES>
+__device__ __forceinline__ void advance(Walk& w, const NormGradParams& p, int ids, int64_t step) {
+  if (w.left == 0) return;
   w.row += p.splits;
-  settle(w, p, ids);
+  w.at += step;
+  if (--w.left == 0 && GATES) {
+    w.unit += ids;
+    start_unit<GATES>(w, p, ids);
+  }
 }
 
 __device__ __forceinline__ float2 pair_of(const float (&x)[8], int i) { return {x[2 * i], x[2 * i + 1]}; }
 __device__ __forceinline__ float2 both(float x) { return {x, x}; }
+
+// Three sums of a warp in six exchanges instead of fifteen: the first two of them halve what a lane carries. Lanes 0-7 end with the
+// first, 16-23 with the second, 8-15 and 24-31 with the third.
+__device__ __forceinline__ float warp_sums3(float a, float b, float c) {
+  const int lane = threadIdx.x & 31;
+  const bool high = lane & 16, third = lane & 8;
+  const float ab = (high ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, high ? a : b, 16);
+  c += __shfl_xor_sync(0xFFFFFFFFu, c, 16);
+  float s = (third ? c : ab) + __shfl_xor_sync(0xFFFFFFFFu, third ? ab : c, 8);
+#pragma unroll
+  for (int d = 4; d > 0; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  return s;
+}
 
 // The two means of the formulas hang on each other: mean(q d v) needs d, which needs mean(w_pre d_y u). Written out,
 //   sum q d v = sum q v (d_o + rstd w_pre d_y) - rstd mean(w_pre d_y u) sum q v u,
 // so one exchange of three sums does. They are taken a row ahead: between two barriers a group of threads sums its next row and writes the
 // outputs of the present one, reading its inputs from shared memory a second time instead of keeping them. (With the sums of a row, a
 // barrier and its outputs in turn: 279 us for 16384 x 4096 bf16.)
-template <int DT, int TPR, bool PRUNE>
+//
+// GATES: a slot's rows have more than one gate, so gates go along with the rows. Else q = g w_post stays in registers, and a thread has
+// room for NV = 2 vectors, TPR threads apart: half the exchanges, addresses and barriers an element.
+template <int DT, int TPR, int NV, bool GATES, bool ALIGNED, bool PRUNE>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 256 ? 1 : 2)
 norm_grad_kernel(const NormGradParams p) {
   using E = Element<DT>;
-  using R = Ring<DT, TPR, 4>;
-  constexpr int SLOTS = kCtaThreads<TPR> / TPR, S = R::kStages;
+  using R = Ring<DT, TPR, 4 * NV, 2>;
+  constexpr int SLOTS = kCtaThreads<TPR> / TPR, S = R::kStages, W = TPR / 32;
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float buffer[2 * 3 * SLOTS * (TPR / 32)];
+  __shared__ float buffer[2 * 3 * SLOTS * W];
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
-  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
+  const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR, lane = threadIdx.x & 31;
   const int id = (int)blockIdx.x * SLOTS + slot, ids = (int)gridDim.x * SLOTS;
+  const int64_t step = (int64_t)p.splits * p.C;
   Walk here;
   here.unit = id;
-  here.group = id / p.splits;
-  here.in_group = id - here.group * p.splits;
-  here.row = (int64_t)here.group * p.rows_per_group + here.in_group;
-  settle(here, p, ids);
-  if (here.unit >= p.units) {
+  start_unit<GATES>(here, p, ids);
+  if (here.left <= 0) {
     // no row at all: the sums of this slot are zero
-    const Part none = part_of(0, p.C, t);
     const float zero[8] = {};
-    if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, none, zero);
-    if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, none, zero);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const Part none = part_of(0, p.C, t + j * TPR);
+      if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, none, zero);
+      if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, none, zero);
+    }
     return;
   }
-  const Part part = part_of(here.row, p.C, t);
+  Part part[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) part[j] = part_of(here.row, p.C, t + j * TPR);
   uint8_t* mine = ring + threadIdx.x * 16;
   const uint32_t mine_u32 = ptx::smem_u32(mine);
   auto fetch = [&](const Walk& w, int stage) {
-    if (w.unit < p.units) {
-      const uint32_t at = mine_u32 + stage * R::kStage;
-      copy_part<DT, R::kChunk>(at, p.branch, w.row, p.C, part);
-      if (p.d_out) copy_part<DT, R::kChunk>(at + R::kVec, p.d_out, w.row, p.C, part);
-      if (p.d_y) {
-        copy_part<DT, R::kChunk>(at + 2 * R::kVec, p.out, w.row, p.C, part);
-        copy_part<DT, R::kChunk>(at + 3 * R::kVec, p.d_y, w.row, p.C, part);
+    if (w.left > 0) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const uint32_t at = mine_u32 + stage * R::kStage + j * 4 * R::kVec;
+        copy_part<DT, R::kChunk>(at, p.branch, w.at, part[j]);
+        if (p.d_out) copy_part<DT, R::kChunk>(at + R::kVec, p.d_out, w.at, part[j]);
+        if (p.d_y) {
+          copy_part<DT, R::kChunk>(at + 2 * R::kVec, p.out, w.at, part[j]);
+          copy_part<DT, R::kChunk>(at + 3 * R::kVec, p.d_y, w.at, part[j]);
+        }
       }
     }
     cp_async_commit();
@@ -340,65 +369,81 @@ norm_grad_kernel(const NormGradParams p) {
   // what belongs to a row beside its elements, loaded a row before it is summed
   struct Beside {
     float rstd_b, rstd;
-    typename E::Raw gate;
+    typename E::Raw gate;  // GATES only
   };
   auto load_beside = [&](const Walk& w, int known_group, Beside& b) {
-    if (w.unit >= p.units) return;
+    if (w.left <= 0) return;
     b.rstd_b = p.post_weight ? p.post_rstd[w.row] : 1.0f;
     b.rstd = p.d_y ? p.pre_rstd[w.row] : 0.0f;
-    if (w.group != known_group) b.gate = column_part<DT>(p.gate, p.gate ? (int64_t)w.group * p.C : 0, part);
+    if (GATES && w.group != known_group) b.gate = column_part<DT>(p.gate, (int64_t)w.group * p.C, part[0]);
   };
-  const typename E::Raw w_post = column_part<DT>(p.post_weight, 0, part), w_pre = column_part<DT>(p.pre_weight, 0, part);
-  auto factors = [&](const Beside& beside, float (&q)[8]) {  // q = g w_post
-    float w[8];
-    E::widen(beside.gate, q);
-    E::widen(w_post, w);
+  typename E::Raw w_post[NV];
+  float q_kept[NV][8], w_kept[NV][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] *= w[e];
-  };
-  const float inv_c = 1.0f / (float)p.C;
-  auto sum_row = [&](const Beside& beside, int stage, int turn) {
-    const uint8_t* at = mine + stage * R::kStage;
-    float b[8], q[8], d[8];
-    read_part<DT, R::kChunk>(at, part, b);
-    factors(beside, q);
-    float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
-    if (p.d_out) {
-      read_part<DT, R::kChunk>(at + R::kVec, part, d);
+  for (int j = 0; j < NV; ++j) {
+    if constexpr (GATES) {
+      w_post[j] = column_part<DT>(p.post_weight, 0, part[j]);
+    } else {
+      float w[8];
+      E::widen(column_part<DT>(p.gate, p.gate ? (int64_t)here.group * p.C : 0, part[j]), q_kept[j]);
+      E::widen(column_part<DT>(p.post_weight, 0, part[j]), w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q_kept[j][e] *= w[e];
+    }
+    E::widen(column_part<DT>(p.pre_weight, 0, part[j]), w_kept[j]);
+  }
+  auto factors = [&](const Beside& beside, int j, float (&q)[8]) {  // q = g w_post
+    if constexpr (GATES) {
+      float w[8];
+      E::widen(beside.gate, q);
+      E::widen(w_post[j], w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[e] *= w[e];
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = 0.0f;
+      for (int e = 0; e < 8; ++e) q[e] = q_kept[j][e];
     }
-    if (p.d_y) {
-      float o[8], y[8], w[8];
-      read_part<DT, R::kChunk>(at + 2 * R::kVec, part, o);
-      read_part<DT, R::kChunk>(at + 3 * R::kVec, part, y);
-      E::widen(w_pre, w);
+  };
+  const float inv_c = 1.0f / (float)p.C;
+  auto sum_row = [&](const Beside& beside, int stage, int turn) -> float {
+    float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const uint8_t* at = mine + stage * R::kStage + j * 4 * R::kVec;
+      float b[8], q[8], d[8];
+      read_part<DT, R::kChunk, ALIGNED>(at, part[j], b);
+      factors(beside, j, q);
+      float o[8], y[8];
+      read_part<DT, R::kChunk, ALIGNED>(at + R::kVec, part[j], d);
+      read_part<DT, R::kChunk, ALIGNED>(at + 2 * R::kVec, part[j], o);
+      read_part<DT, R::kChunk, ALIGNED>(at + 3 * R::kVec, part[j], y);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 wd = mul2(pair_of(y, i), pair_of(w, i)), qb = mul2(pair_of(q, i), pair_of(b, i));
+        const float2 wd = mul2(pair_of(y, i), pair_of(w_kept[j], i)), qb = mul2(pair_of(q, i), pair_of(b, i));
         s0 = fma2(wd, pair_of(o, i), s0);
         s1 = fma2(qb, fma2(both(beside.rstd), wd, pair_of(d, i)), s1);
         s2 = fma2(qb, pair_of(o, i), s2);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s1 = fma2(mul2(pair_of(q, i), pair_of(b, i)), pair_of(d, i), s1);
     }
-    float s[3] = {beside.rstd * (s0.x + s0.y), beside.rstd_b * (s1.x + s1.y), beside.rstd_b * beside.rstd * (s2.x + s2.y)};
-    float* to = buffer + (turn * SLOTS + slot) * (TPR / 32) * 3;
-    put_sums<TPR>(s, to);
-    return make_float3(s[0], s[1], s[2]);  // (rows of one warp: these are the sums)
+    const float s = warp_sums3(beside.rstd * (s0.x + s0.y), beside.rstd_b * (s1.x + s1.y), beside.rstd_b * beside.rstd * (s2.x + s2.y));
+    if (TPR > 32 && (lane & 7) == 0 && lane != 24) buffer[(turn * SLOTS + slot) * W * 3 + (lane == 0 ? 0 : lane == 16 ? W : 2 * W) + (t >> 5)] = s;
+    return s;
   };
 
+  // tensors that are absent are zeros
+  for (int v = 0; v < 4 * NV * S; ++v) {
+    if (v % 4 == 0 || (v % 4 == 1 ? p.d_out : p.d_y) != nullptr) continue;
+    *(uint4*)(mine + v * R::kVec) = make_uint4(0u, 0u, 0u, 0u);
+    if (E::k32) *(uint4*)(mine + v * R::kVec + R::kChunk) = make_uint4(0u, 0u, 0u, 0u);
+  }
   Walk next = here;
-  advance(next, p, ids);
+  advance<GATES>(next, p, ids, step);
   Walk after = next, ahead = here;
-  advance(after, p, ids);
+  advance<GATES>(after, p, ids, step);
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     fetch(ahead, s);
-    advance(ahead, p, ids);
+    advance<GATES>(ahead, p, ids, step);
   }
   Beside beside = {}, beside_next = {}, beside_after = {};
   load_beside(here, -1, beside);
@@ -406,89 +451,110 @@ norm_grad_kernel(const NormGradParams p) {
   load_beside(next, here.group, beside_next);
   beside_after = beside_next;
   cp_async_wait<S - 1>();
-  float3 own = sum_row(beside, 0, 0), own_next = own;
+  float own = sum_row(beside, 0, 0), own_next = own;
   if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
 
-  float2 pre_sum[4] = {}, post_sum[4] = {}, gate_sum[4] = {};
+  float2 pre_sum[NV][4] = {}, post_sum[NV][4] = {}, gate_sum[NV][4] = {};
   int stage = 0, turn = 0;
-  while (here.unit < p.units) {
+  while (here.left > 0) {
     const int stage_next = stage + 1 == S ? 0 : stage + 1;
     load_beside(after, next.group, beside_after);
-    if (next.unit < p.units) {
-      cp_async_wait<(S > 1 ? S - 2 : 0)>();
+    if (next.left > 0) {
+      cp_async_wait<S - 2>();
       own_next = sum_row(beside_next, stage_next, turn ^ 1);
     }
-    float s[3] = {own.x, own.y, own.z};
-    get_sums<TPR>(s, buffer + (turn * SLOTS + slot) * (TPR / 32) * 3);
-    const float k = beside.rstd * (s[0] * inv_c), mean = (s[1] - k * s[2]) * inv_c;
-    const uint8_t* at = mine + stage * R::kStage;
-    float b[8], q[8], d[8];
-    read_part<DT, R::kChunk>(at, part, b);
-    if (p.d_out) {
-      read_part<DT, R::kChunk>(at + R::kVec, part, d);
+    float s0, s1, s2;
+    if constexpr (TPR > 32) {
+      const float* from = buffer + (turn * SLOTS + slot) * W * 3 + lane % W;
+      s0 = sum_lanes<W>(from[0]);
+      s1 = sum_lanes<W>(from[W]);
+      s2 = sum_lanes<W>(from[2 * W]);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = 0.0f;
+      s0 = __shfl_sync(0xFFFFFFFFu, own, 0);
+      s1 = __shfl_sync(0xFFFFFFFFu, own, 16);
+      s2 = __shfl_sync(0xFFFFFFFFu, own, 8);
     }
-    if (p.d_y) {
-      float o[8], y[8], w[8];
-      read_part<DT, R::kChunk>(at + 2 * R::kVec, part, o);
-      read_part<DT, R::kChunk>(at + 3 * R::kVec, part, y);
-      E::widen(w_pre, w);
+    const float k = beside.rstd * (s0 * inv_c), mean = (s1 - k * s2) * inv_c;
+    const bool unit_ends = here.left == 1;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const uint8_t* at = mine + stage * R::kStage + j * 4 * R::kVec;
+      float b[8], q[8], d[8], out[8];
+      read_part<DT, R::kChunk, ALIGNED>(at, part[j], b);
+      float o[8], y[8];
+      read_part<DT, R::kChunk, ALIGNED>(at + R::kVec, part[j], d);
+      read_part<DT, R::kChunk, ALIGNED>(at + 2 * R::kVec, part[j], o);
+      read_part<DT, R::kChunk, ALIGNED>(at + 3 * R::kVec, part[j], y);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 dy = pair_of(y, i), u = mul2(pair_of(o, i), both(beside.rstd));
-        pre_sum[i] = fma2(dy, u, pre_sum[i]);
-        const float2 x = fma2(both(-k), u, fma2(both(beside.rstd), mul2(dy, pair_of(w, i)), pair_of(d, i)));
+        pre_sum[j][i] = fma2(dy, u, pre_sum[j][i]);
+        const float2 x = fma2(both(-k), u, fma2(both(beside.rstd), mul2(dy, pair_of(w_kept[j], i)), pair_of(d, i)));
         d[2 * i] = x.x;
         d[2 * i + 1] = x.y;
       }
-    }
-    float out[8];
-    if (p.d_residual) {
+      if (p.d_residual) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) out[e] = p.alpha * d[e];
-      write_part<DT>(p.d_residual, here.row, p.C, part, E::narrow(out), out);
-    }
-    factors(beside, q);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 x = pair_of(d, i), v = mul2(pair_of(b, i), both(beside.rstd_b));
-      gate_sum[i] = fma2(x, v, gate_sum[i]);
-      float2 y = mul2(pair_of(q, i), x);
-      if (p.post_weight) y = mul2(fma2(v, both(-mean), y), both(beside.rstd_b));
-      out[2 * i] = y.x;
-      out[2 * i + 1] = y.y;
-    }
-    const typename E::Raw packed = E::narrow(out);
-    if (p.d_branch) write_part<DT>(p.d_branch, here.row, p.C, part, packed, out);
-    if constexpr (PRUNE) {  // (rows of whole groups of 16: every part is full or empty, and a group's lanes alike)
-      const int64_t vec = here.row * (p.C / 8) + t;
-      const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, t & 3);
-      if (part.full) {
-        if (p.values) p.values[vec] = make_uint2(c.x, c.y);
-        if (p.meta) p.meta[vec] = (uint8_t)c.z;
+        for (int i = 0; i < 4; ++i) {
+          const float2 x = mul2(both(p.alpha), pair_of(d, i));
+          out[2 * i] = x.x;
+          out[2 * i + 1] = x.y;
+        }
+        write_part<DT, ALIGNED>(p.d_residual, here.at, part[j], E::narrow(out), out);
       }
-    }
-    if (here.unit != next.unit) {  // the unit's rows are done: sum of d v over them
-      float g[8], w[8];
-      E::widen(beside.gate, g);
-      E::widen(w_post, w);
+      factors(beside, j, q);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        post_sum[i] = fma2(pair_of(g, i), gate_sum[i], post_sum[i]);
-        out[2 * i] = w[2 * i] * gate_sum[i].x;
-        out[2 * i + 1] = w[2 * i + 1] * gate_sum[i].y;
-        gate_sum[i] = both(0.0f);
+        const float2 x = pair_of(d, i), v = mul2(pair_of(b, i), both(beside.rstd_b));
+        gate_sum[j][i] = fma2(x, v, gate_sum[j][i]);
+        float2 y = mul2(pair_of(q, i), x);
+        if (p.post_weight) y = mul2(fma2(v, both(-mean), y), both(beside.rstd_b));
+        out[2 * i] = y.x;
+        out[2 * i + 1] = y.y;
       }
-      if (p.gate_sums) write_sums(p.gate_sums + ((int64_t)here.group * p.gate_rows + (here.unit - here.group * p.splits)) * p.C, part, out);
-      else if (p.d_gate) write_sums(p.d_gate + (int64_t)here.group * p.C, part, out);
+      const typename E::Raw packed = E::narrow(out);
+      if (p.d_branch) write_part<DT, ALIGNED>(p.d_branch, here.at, part[j], packed, out);
+      if constexpr (PRUNE) {  // (rows of whole groups of 16: every part is full or empty, and a group's lanes alike)
+        const int64_t vec = (here.at >> 3) + t + j * TPR;
+        const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, t & 3);
+        if (part[j].full) {
+          if (p.values) p.values[vec] = make_uint2(c.x, c.y);
+          if (p.meta) p.meta[vec] = (uint8_t)c.z;
+        }
+      }
+      if (unit_ends) {  // sum of d v over the unit's rows, times g for d_w_post and times w_post for d_g
+        float g[8], w[8];
+        if constexpr (GATES) {
+          E::widen(beside.gate, g);
+          E::widen(w_post[j], w);
+        } else {
+          E::widen(column_part<DT>(p.gate, p.gate ? (int64_t)here.group * p.C : 0, part[j]), g);
+          E::widen(column_part<DT>(p.post_weight, 0, part[j]), w);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          post_sum[j][i] = GATES ? fma2(pair_of(g, i), gate_sum[j][i], post_sum[j][i]) : mul2(pair_of(g, i), gate_sum[j][i]);
+          out[2 * i] = w[2 * i] * gate_sum[j][i].x;
+          out[2 * i + 1] = w[2 * i + 1] * gate_sum[j][i].y;
+          gate_sum[j][i] = both(0.0f);
+        }
+        if (p.gate_sums) write_sums(p.gate_sums + ((int64_t)here.group * p.gate_rows + (here.unit - here.group * p.splits)) * p.C, part[j], out);
+        else if (p.d_gate) write_sums(p.d_gate + (int64_t)here.group * p.C, part[j], out);
+        if (!GATES && p.post_sums) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            out[2 * i] = post_sum[j][i].x;
+            out[2 * i + 1] = post_sum[j][i].y;
+          }
+          write_sums(p.post_sums + (int64_t)id * p.C, part[j], out);
+        }
+      }
     }
     fetch(ahead, stage);
-    advance(ahead, p, ids);
+    advance<GATES>(ahead, p, ids, step);
     here = next;
     next = after;
-    advance(after, p, ids);
+    advance<GATES>(after, p, ids, step);
     beside = beside_next;
     beside_next = beside_after;
     own = own_next;
@@ -497,19 +563,24 @@ norm_grad_kernel(const NormGradParams p) {
     if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
   }
   cp_async_wait<0>();
-  float x[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = pre_sum[i].x;
-    x[2 * i + 1] = pre_sum[i].y;
-  }
-  if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, part, x);
+  for (int j = 0; j < NV; ++j) {
+    float x[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = post_sum[i].x;
-    x[2 * i + 1] = post_sum[i].y;
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = pre_sum[j][i].x;
+      x[2 * i + 1] = pre_sum[j][i].y;
+    }
+    if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, part[j], x);
+    if (GATES && p.post_sums) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = post_sum[j][i].x;
+        x[2 * i + 1] = post_sum[j][i].y;
+      }
+      write_sums(p.post_sums + (int64_t)id * p.C, part[j], x);
+    }
   }
-  if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, part, x);
 }
 
 // Sums of the slots' sums, in a fixed order. Job 0: d_pre_weight, 1: d_post_weight, 2 + g: gate g.
@@ -619,12 +690,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_wide_kernel(const NormPa
       const Part part = part_of(row, p.C, j);
       float o[8], w[8];
       sums_of(part, o);
-      write_part<DT>(p.out, row, p.C, part, E::narrow(o), o);
+      write_part<DT>(p.out, row * p.C, part, E::narrow(o), o);
       if (p.pre_weight) {
         load_columns<DT>(p.pre_weight, 0, part, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = o[e] * rstd * w[e];
-        write_part<DT>(p.y, row, p.C, part, E::narrow(o), o);
+        write_part<DT>(p.y, row * p.C, part, E::narrow(o), o);
       }
     }
   }
@@ -701,7 +772,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
           d[e] = fmaf(-k, u[e], d[e]);
           x[e] = p.alpha * d[e];
         }
-        if (p.d_residual) write_part<DT>(p.d_residual, row, p.C, part, E::narrow(x), x);
+        if (p.d_residual) write_part<DT>(p.d_residual, row * p.C, part, E::narrow(x), x);
         if (p.post_sums) {
           load_columns<DT>(p.gate, (int64_t)group * p.C, part, w);
 #pragma unroll
@@ -717,7 +788,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = p.post_weight ? rstd_b * fmaf(q[e], d[e], -v[e] * mean) : q[e] * d[e];
         const typename E::Raw packed = E::narrow(x);
-        if (p.d_branch) write_part<DT>(p.d_branch, row, p.C, part, packed, x);
+        if (p.d_branch) write_part<DT>(p.d_branch, row * p.C, part, packed, x);
         if constexpr (PRUNE) {
           const int64_t vec = row * (p.C / 8) + j;
           const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, j & 3);
@@ -744,35 +815,46 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
 
 int gcd8(int c) { return c % 8 == 0 ? 8 : c % 4 == 0 ? 4 : c % 2 == 0 ? 2 : 1; }
 
-// Threads of a row: the smallest power of two from 32 to 1024 whose vectors hold it at any place that it may start at; 0: the wide kernels.
-int threads_of_row(int64_t C) {
-  for (int t = 32; t <= 1024; t *= 2)
-    if (C + 8 - gcd8((int)(C % 8)) <= 8 * t) return t;
+// Threads of a row of `vectors` vectors each: the smallest power of two from 32 to `most` that holds it at any place that it may start
+// at; 0: the wide kernels.
+int threads_of_row(int64_t C, int vectors, int most) {
+  for (int t = 32; t <= most; t *= 2)
+    if (C + 8 - gcd8((int)(C % 8)) <= 8 * vectors * t) return t;
   return 0;
 }
 
 struct Plan {
-  int tpr, slots_per_cta, ctas, period, splits, units, gate_rows;
+  int tpr, vectors, slots_per_cta, ctas, period, splits, units, gate_rows;
+  bool gates;  // a slot's rows may have several gates: the kernel that carries them along
   int ids() const { return ctas * slots_per_cta; }
 };
 
 // How rows are dealt to slots (groups of threads). All rows of a slot start at the same place of a vector: they are multiples of the period
-// apart. groups == 0: the forward pass, rows at the stride of all slots.
-Plan plan_rows(int64_t rows, int64_t C, int64_t groups, int ctas_per_sm) {
+// apart.
+Plan plan_slots(int64_t rows, int64_t C, int tpr, int ctas_per_sm) {
   Plan p = {};
-  p.tpr = threads_of_row(C);
-  p.slots_per_cta = p.tpr == 0 || p.tpr >= 256 ? 1 : 256 / p.tpr;
+  p.tpr = tpr;
+  p.vectors = 1;
+  p.slots_per_cta = tpr == 0 || tpr >= 256 ? 1 : 256 / tpr;
   p.period = 8 / gcd8((int)(C % 8));
-  const int64_t most = (int64_t)sm_count() * ctas_per_sm;
-  const int64_t wanted = (rows + p.slots_per_cta - 1) / p.slots_per_cta;
-  int64_t ctas = wanted < most ? wanted : most;
-  if (groups == 0) {
-    if (ctas < wanted && p.period > p.slots_per_cta) ctas -= ctas % (p.period / p.slots_per_cta);
-    p.ctas = (int)ctas;
-    return p;
-  }
+  const int64_t most = (int64_t)sm_count() * ctas_per_sm, wanted = (rows + p.slots_per_cta - 1) / p.slots_per_cta;
+  p.ctas = (int)(wanted < most ? wanted : most);
+  return p;
+}
+
+// Forward: rows at the stride of all slots.
+Plan forward_plan(int64_t rows, int64_t C) {
+  const int tpr = threads_of_row(C, 1, 1024);
+  Plan p = plan_slots(rows, C, tpr, tpr == 0 ? 2 : tpr > 512 ? 1 : tpr > 256 ? 2 : 4);
+  if (p.ids() < rows && p.period > p.slots_per_cta) p.ctas -= p.ctas % (p.period / p.slots_per_cta);
+  return p;
+}
+
+// Backward: rows in units of one gate.
+Plan deal_units(Plan p, int64_t rows, int64_t groups) {
   const int64_t per_group = rows / groups;
-  int64_t ids = ctas * p.slots_per_cta;
+  int64_t ctas = p.ctas;
+  const int64_t ids = ctas * p.slots_per_cta;
   int64_t splits = ids / groups;
   splits -= splits % p.period;
   if (splits < p.period) splits = per_group == 1 || p.period == 1 ? 1 : p.period;
@@ -790,11 +872,24 @@ Plan plan_rows(int64_t rows, int64_t C, int64_t groups, int ctas_per_sm) {
     ctas = (p.units + p.slots_per_cta - 1) / p.slots_per_cta;
   }
   p.ctas = (int)ctas;
+  p.gates = p.units > p.ids();
   return p;
 }
 
-constexpr int kForwardCtasPerSm(int tpr) { return tpr == 0 ? 2 : tpr > 512 ? 1 : tpr > 256 ? 2 : 4; }
-constexpr int kBackwardCtasPerSm(int tpr) { return tpr == 0 ? 1 : tpr > 256 ? 1 : 2; }
+Plan backward_plan(int64_t rows, int64_t C, int64_t groups, bool fp32) {
+  // one gate a slot: two vectors a thread (fp32: shared memory holds the stages of one)
+  const int vectors = fp32 ? 1 : 2;
+  int tpr = threads_of_row(C, vectors, 512);
+  if (tpr != 0) {
+    Plan p = deal_units(plan_slots(rows, C, tpr, tpr > 256 ? 1 : 2), rows, groups);
+    p.vectors = vectors;
+    if (!p.gates) return p;
+  }
+  tpr = threads_of_row(C, 1, fp32 ? 512 : 1024);
+  Plan p = deal_units(plan_slots(rows, C, tpr, tpr == 0 || tpr > 256 ? 1 : 2), rows, groups);
+  p.gates = tpr != 0;
+  return p;
+}
 
 template <auto Kernel, typename... Args>
 cudaError_t launch(int64_t ctas, dim3 block, int smem, cudaStream_t stream, const Args&... args) {
@@ -824,26 +919,43 @@ template <int DT>
 cudaError_t launch_forward(const NormParams& p, const Plan& plan, cudaStream_t stream) {
   switch (plan.tpr) {
 #define SDGP_ROW(T) \
-  case T: return launch<norm_kernel<DT, T>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 2>::kBytes, stream, p);
+  case T: return launch<norm_kernel<DT, T>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 2, 1>::kBytes, stream, p);
     SDGP_ROW(32) SDGP_ROW(64) SDGP_ROW(128) SDGP_ROW(256) SDGP_ROW(512) SDGP_ROW(1024)
 #undef SDGP_ROW
   }
   return launch<norm_wide_kernel<DT>>(plan.ctas, dim3(kWideThreads), 0, stream, p);
 }
 
-template <int DT, bool PRUNE>
-cudaError_t launch_backward(const NormGradParams& p, const Plan& plan, cudaStream_t stream) {
-  // (fp32 rows of 1024 threads leave room for one stage only, and a row ahead needs two)
-  switch (DT == SDGP_FP32 && plan.tpr == 1024 ? 0 : plan.tpr) {
-#define SDGP_ROW(T) \
-  case T: return launch<norm_grad_kernel<DT, T, PRUNE>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 4>::kBytes, stream, p);
-    SDGP_ROW(32) SDGP_ROW(64) SDGP_ROW(128) SDGP_ROW(256) SDGP_ROW(512) SDGP_ROW(1024)
-#undef SDGP_ROW
+template <int DT, bool ALIGNED, bool PRUNE>
+cudaError_t launch_backward_form(const NormGradParams& p, const Plan& plan, cudaStream_t stream) {
+#define SDGP_ROW(T, NV, GATES)                                                                                                      \
+  case T: return launch<norm_grad_kernel<DT, T, NV, GATES, ALIGNED, PRUNE>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 4 * NV, 2>::kBytes, \
+                                                                             stream, p);
+  if (!plan.gates) {
+    constexpr int NV = DT == SDGP_FP32 ? 1 : 2;
+    if (plan.vectors == NV) {
+      switch (plan.tpr) { SDGP_ROW(32, NV, false) SDGP_ROW(64, NV, false) SDGP_ROW(128, NV, false) SDGP_ROW(256, NV, false) SDGP_ROW(512, NV, false) }
+    }
+  } else {
+    switch (plan.tpr) {
+      SDGP_ROW(32, 1, true) SDGP_ROW(64, 1, true) SDGP_ROW(128, 1, true) SDGP_ROW(256, 1, true) SDGP_ROW(512, 1, true)
+    }
+    if constexpr (DT != SDGP_FP32) {
+      switch (plan.tpr) { SDGP_ROW(1024, 1, true) }
+    }
   }
+#undef SDGP_ROW
   return launch<norm_grad_wide_kernel<DT, PRUNE>>(plan.ctas, dim3(kWideThreads), 0, stream, p);
 }
 
-Plan backward_plan(int64_t rows, int64_t C, int64_t groups) { return plan_rows(rows, C, groups, kBackwardCtasPerSm(threads_of_row(C))); }
+template <int DT>
+cudaError_t launch_backward(const NormGradParams& p, const Plan& plan, cudaStream_t stream) {
+  if (plan.period != 1) return launch_backward_form<DT, false, false>(p, plan, stream);
+  if constexpr (DT != SDGP_FP32) {
+    if (p.values || p.meta) return launch_backward_form<DT, true, true>(p, plan, stream);
+  }
+  return launch_backward_form<DT, true, false>(p, plan, stream);
+}
 
 }  // namespace
 
@@ -852,15 +964,22 @@ cudaError_t launch_residual_norm(const void* branch, const void* residual, const
                                  float* post_rstd, float* pre_rstd, cudaStream_t stream) {
   const NormParams p = {branch, residual, post_weight, gate, pre_weight, out, y, post_rstd, pre_rstd, rows, rows / groups, (int)C, (int)groups,
                         alpha, eps};
-  const Plan plan = plan_rows(rows, C, 0, kForwardCtasPerSm(threads_of_row(C)));
+  const Plan plan = forward_plan(rows, C);
   if (dtype == SDGP_BF16) return launch_forward<SDGP_BF16>(p, plan, stream);
   if (dtype == SDGP_FP16) return launch_forward<SDGP_FP16>(p, plan, stream);
   return launch_forward<SDGP_FP32>(p, plan, stream);
 }
 
 size_t residual_norm_backward_floats(int64_t rows, int64_t C, int64_t groups) {
-  const Plan plan = backward_plan(rows, C, groups);
-  return (size_t)C * (2 * (size_t)plan.ids() + (plan.splits > 1 ? (size_t)groups * plan.gate_rows : 0));
+  size_t most = 0;
+  for (const int64_t g : {groups, (int64_t)1}) {  // (1: a call without gates)
+    for (const bool fp32 : {false, true}) {
+      const Plan plan = backward_plan(rows, C, g, fp32);
+      const size_t n = (size_t)C * (2 * (size_t)plan.ids() + (plan.splits > 1 ? (size_t)g * plan.gate_rows : 0));
+      if (n > most) most = n;
+    }
+  }
+  return most;
 }
 
 cudaError_t launch_residual_norm_backward(const void* branch, const void* out, const void* d_out, const void* d_y, const void* post_weight,
@@ -868,18 +987,17 @@ cudaError_t launch_residual_norm_backward(const void* branch, const void* out, c
                                           int64_t rows, int64_t C, int64_t groups, float alpha, int n, int m, int scheme, uint64_t seed,
                                           int dtype, void* d_residual, void* d_branch, float* d_gate, float* d_post_weight,
                                           float* d_pre_weight, void* values, void* meta, float* workspace, cudaStream_t stream) {
-  const Plan plan = backward_plan(rows, C, groups);
+  if (!gate) groups = 1;
+  const Plan plan = backward_plan(rows, C, groups, dtype == SDGP_FP32);
   float* pre_sums = d_pre_weight ? workspace : nullptr;
   float* post_sums = d_post_weight ? workspace + (size_t)plan.ids() * C : nullptr;
   float* gate_sums = d_gate && plan.splits > 1 ? workspace + 2 * (size_t)plan.ids() * C : nullptr;
   const NormGradParams p = {branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, d_residual, d_branch,
                             (uint2*)values, (uint8_t*)meta, d_gate, pre_sums, post_sums, gate_sums, rows, rows / groups, (int)C,
                             plan.splits, plan.units, plan.gate_rows, alpha, n, m, scheme, (uint32_t)seed, (uint32_t)(seed >> 32)};
-  const bool prune = values || meta;
-  cudaError_t e;
-  if (dtype == SDGP_FP32) e = launch_backward<SDGP_FP32, false>(p, plan, stream);
-  else if (dtype == SDGP_BF16) e = prune ? launch_backward<SDGP_BF16, true>(p, plan, stream) : launch_backward<SDGP_BF16, false>(p, plan, stream);
-  else e = prune ? launch_backward<SDGP_FP16, true>(p, plan, stream) : launch_backward<SDGP_FP16, false>(p, plan, stream);
+  const cudaError_t e = dtype == SDGP_BF16   ? launch_backward<SDGP_BF16>(p, plan, stream)
+                        : dtype == SDGP_FP16 ? launch_backward<SDGP_FP16>(p, plan, stream)
+                                             : launch_backward<SDGP_FP32>(p, plan, stream);
   if (e != cudaSuccess || (!pre_sums && !post_sums && !gate_sums)) return e;
   const SumParams q = {pre_sums, post_sums, gate_sums, d_pre_weight, d_post_weight, d_gate, (int)C, plan.ids(), plan.gate_rows};
   const int64_t jobs = 2 + (gate_sums ? groups : 0);

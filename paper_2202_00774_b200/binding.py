@@ -295,7 +295,7 @@ def sdgp_residual_norm(branch, residual, out, y=None, post_weight=None, gate=Non
 
 
 def sdgp_workspace_size_residual_norm_backward(rows, C, groups=1) -> int:
-    return int(lib().sdgp_workspace_size_residual_norm_backward(rows, C, groups))
+    return (_torch or _load()).workspace_size_residual_norm_backward(rows, C, groups)
 
 
 def sdgp_residual_norm_backward(branch, out, d_out, d_y=None, post_weight=None, gate=None, pre_weight=None, post_rstd=None, pre_rstd=None,

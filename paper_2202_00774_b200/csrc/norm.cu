@@ -106,7 +106,7 @@ __device__ __forceinline__ typename Element<DT>::Raw column_part(const void* src
   for (int e = 0; e < 8; ++e) x[e] = !src ? 1.0f : e >= p.lo && e < p.hi ? E::load(src, offset + p.first + e) : 0.0f;
   return E::narrow(x);
 }
-__device__ __forceinline__ void write_sums(float* dst, const Part& p, const float (&x)[8]) {
+__device__ __forceinline__ void write_columns(float* dst, const Part& p, const float (&x)[8]) {
   if (p.full && ((uintptr_t)(dst + p.first) & 15u) == 0) {
     *(float4*)(dst + p.first) = make_float4(x[0], x[1], x[2], x[3]);
     *(float4*)(dst + p.first + 4) = make_float4(x[4], x[5], x[6], x[7]);
@@ -237,10 +237,12 @@ struct NormGradParams {
   uint2* values;                                // compressed pruned copy of d_branch; each optional
   uint8_t* meta;
   float* d_gate;                                // [groups, C]; optional
-  // sums over the rows of one group of threads: [slots, C], or null where nobody asks for them; of the rows of one unit: [groups, gate_rows, C]
-  float *pre_sums, *post_sums, *gate_sums;
+  // Sums over a slot's rows of d_y u and of d g v, [slots, pitch], and over a unit's rows of d v, [groups, gate_rows, pitch]; null where they
+  // are not needed (post_sums: only with GATES; else the sums of d v give d_w_post too). A row of sums is laid out as its rows are in their
+  // vectors: column c at c + (place of the first row in its vector), so that threads write whole vectors.
+  float *pre_sums, *post_sums, *unit_sums;
   int64_t rows, rows_per_group;
-  int C, splits, units, gate_rows;  // gate_rows: units of a gate that have rows
+  int C, pitch, splits, units, gate_rows;  // gate_rows: units of a gate that have rows
   float alpha;
   int n, m, scheme;
   uint32_t seed_lo, seed_hi;
@@ -298,6 +300,11 @@ __device__ __forceinline__ void advance(Walk& w, const NormGradParams& p, int id
 __device__ __forceinline__ float2 pair_of(const float (&x)[8], int i) { return {x[2 * i], x[2 * i + 1]}; }
 __device__ __forceinline__ float2 both(float x) { return {x, x}; }
 
+__device__ __forceinline__ void write_sums(float* dst, const float2 (&x)[4]) {
+  *(float4*)dst = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+  *(float4*)(dst + 4) = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+}
+
 // Three sums of a warp in six exchanges instead of fifteen: the first two of them halve what a lane carries. Lanes 0-7 end with the
 // first, 16-23 with the second, 8-15 and 24-31 with the third.
 __device__ __forceinline__ float warp_sums3(float a, float b, float c) {
@@ -337,12 +344,12 @@ norm_grad_kernel(const NormGradParams p) {
   start_unit<GATES>(here, p, ids);
   if (here.left <= 0) {
     // no row at all: the sums of this slot are zero
-    const float zero[8] = {};
+    const float2 zero[4] = {};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const Part none = part_of(0, p.C, t + j * TPR);
-      if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, none, zero);
-      if (p.post_sums) write_sums(p.post_sums + (int64_t)id * p.C, none, zero);
+      const int at = (t + j * TPR) * 8;
+      if (at < p.pitch && p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.pitch + at, zero);
+      if (at < p.pitch && p.post_sums) write_sums(p.post_sums + (int64_t)id * p.pitch + at, zero);
     }
     return;
   }
@@ -377,21 +384,8 @@ norm_grad_kernel(const NormGradParams p) {
     b.rstd = p.d_y ? p.pre_rstd[w.row] : 0.0f;
     if (GATES && w.group != known_group) b.gate = column_part<DT>(p.gate, (int64_t)w.group * p.C, part[0]);
   };
-  typename E::Raw w_post[NV];
+  typename E::Raw w_post[NV], raw_gate[NV], raw_pre[NV];
   float q_kept[NV][8], w_kept[NV][8];
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if constexpr (GATES) {
-      w_post[j] = column_part<DT>(p.post_weight, 0, part[j]);
-    } else {
-      float w[8];
-      E::widen(column_part<DT>(p.gate, p.gate ? (int64_t)here.group * p.C : 0, part[j]), q_kept[j]);
-      E::widen(column_part<DT>(p.post_weight, 0, part[j]), w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) q_kept[j][e] *= w[e];
-    }
-    E::widen(column_part<DT>(p.pre_weight, 0, part[j]), w_kept[j]);
-  }
   auto factors = [&](const Beside& beside, int j, float (&q)[8]) {  // q = g w_post
     if constexpr (GATES) {
       float w[8];
@@ -445,11 +439,29 @@ norm_grad_kernel(const NormGradParams p) {
     fetch(ahead, s);
     advance<GATES>(ahead, p, ids, step);
   }
+  // (all loads are under way before the first of them is waited for)
   Beside beside = {}, beside_next = {}, beside_after = {};
   load_beside(here, -1, beside);
-  beside_next = beside;
+  beside_next.gate = beside.gate;
   load_beside(next, here.group, beside_next);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    w_post[j] = column_part<DT>(p.post_weight, 0, part[j]);
+    raw_pre[j] = column_part<DT>(p.pre_weight, 0, part[j]);
+    if (!GATES) raw_gate[j] = column_part<DT>(p.gate, p.gate ? (int64_t)here.group * p.C : 0, part[j]);
+  }
   beside_after = beside_next;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    E::widen(raw_pre[j], w_kept[j]);
+    if constexpr (!GATES) {
+      float w[8];
+      E::widen(raw_gate[j], q_kept[j]);
+      E::widen(w_post[j], w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q_kept[j][e] *= w[e];
+    }
+  }
   cp_async_wait<S - 1>();
   float own = sum_row(beside, 0, 0), own_next = own;
   if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
@@ -522,31 +534,22 @@ norm_grad_kernel(const NormGradParams p) {
           if (p.meta) p.meta[vec] = (uint8_t)c.z;
         }
       }
-      if (unit_ends) {  // sum of d v over the unit's rows, times g for d_w_post and times w_post for d_g
-        float g[8], w[8];
+      if (unit_ends) {  // sum of d v over the unit's rows: times g for d_w_post, times w_post for d_g
+        const bool some = part[j].hi > 0;
+        if (p.unit_sums && some)
+          write_sums(p.unit_sums + ((int64_t)here.group * p.gate_rows + (here.unit - here.group * p.splits)) * p.pitch + (t + j * TPR) * 8, gate_sum[j]);
         if constexpr (GATES) {
+          float g[8], w[8];
           E::widen(beside.gate, g);
           E::widen(w_post[j], w);
-        } else {
-          E::widen(column_part<DT>(p.gate, p.gate ? (int64_t)here.group * p.C : 0, part[j]), g);
-          E::widen(column_part<DT>(p.post_weight, 0, part[j]), w);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          post_sum[j][i] = GATES ? fma2(pair_of(g, i), gate_sum[j][i], post_sum[j][i]) : mul2(pair_of(g, i), gate_sum[j][i]);
-          out[2 * i] = w[2 * i] * gate_sum[j][i].x;
-          out[2 * i + 1] = w[2 * i + 1] * gate_sum[j][i].y;
-          gate_sum[j][i] = both(0.0f);
-        }
-        if (p.gate_sums) write_sums(p.gate_sums + ((int64_t)here.group * p.gate_rows + (here.unit - here.group * p.splits)) * p.C, part[j], out);
-        else if (p.d_gate) write_sums(p.d_gate + (int64_t)here.group * p.C, part[j], out);
-        if (!GATES && p.post_sums) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            out[2 * i] = post_sum[j][i].x;
-            out[2 * i + 1] = post_sum[j][i].y;
+            post_sum[j][i] = fma2(pair_of(g, i), gate_sum[j][i], post_sum[j][i]);
+            out[2 * i] = w[2 * i] * gate_sum[j][i].x;
+            out[2 * i + 1] = w[2 * i + 1] * gate_sum[j][i].y;
+            gate_sum[j][i] = both(0.0f);
           }
-          write_sums(p.post_sums + (int64_t)id * p.C, part[j], out);
+          if (!p.unit_sums && p.d_gate) write_columns(p.d_gate + (int64_t)here.group * p.C, part[j], out);
         }
       }
     }
@@ -565,50 +568,98 @@ norm_grad_kernel(const NormGradParams p) {
   cp_async_wait<0>();
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = pre_sum[j][i].x;
-      x[2 * i + 1] = pre_sum[j][i].y;
-    }
-    if (p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.C, part[j], x);
-    if (GATES && p.post_sums) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[2 * i] = post_sum[j][i].x;
-        x[2 * i + 1] = post_sum[j][i].y;
-      }
-      write_sums(p.post_sums + (int64_t)id * p.C, part[j], x);
-    }
+    if (part[j].hi <= 0) continue;
+    const int64_t at = (int64_t)id * p.pitch + (t + j * TPR) * 8;
+    if (p.pre_sums) write_sums(p.pre_sums + at, pre_sum[j]);
+    if (GATES && p.post_sums) write_sums(p.post_sums + at, post_sum[j]);
   }
 }
 
-// Sums of the slots' sums, in a fixed order. Job 0: d_pre_weight, 1: d_post_weight, 2 + g: gate g.
+// Sums of those sums, in a fixed order. A CTA takes 32 columns: with its 32 lines of threads either one line of sums of the slots each
+// (job 0: d_pre_weight; job 1, with GATES: d_post_weight) or, job 2, groups and their units: d_gate = w_post sum d v of each group and, without
+// GATES, d_post_weight = sum over groups of g sum d v.
 struct SumParams {
-  const float *pre_sums, *post_sums, *gate_sums;
+  const float *pre_sums, *post_sums, *unit_sums;
+  const void *gate, *post_weight;
   float *d_pre_weight, *d_post_weight, *d_gate;
-  int C, slots, gate_rows;
+  int64_t rows_per_group, groups;
+  int C, pitch, slots, splits, gate_rows;
+  bool shifted;  // lines of sums start at the place of their first row in its vector
+  int job0, jobs;
 };
-constexpr int kSumLanes = 16;
-__global__ void __launch_bounds__(32 * kSumLanes) norm_sums_kernel(const SumParams p) {
-  __shared__ float part[kSumLanes][33];
-  ptx::wait_for_previous_grid();
-  ptx::launch_dependents();
-  const int blocks_of_job = (p.C + 31) / 32, job = (int)(blockIdx.x / blocks_of_job), c = (int)(blockIdx.x % blocks_of_job) * 32 + threadIdx.x;
-  const float* src = job == 0 ? p.pre_sums : job == 1 ? p.post_sums : p.gate_sums + (int64_t)(job - 2) * p.gate_rows * p.C;
-  float* dst = job == 0 ? p.d_pre_weight : job == 1 ? p.d_post_weight : p.d_gate + (int64_t)(job - 2) * p.C;
-  if (!src) return;
-  const int n = job < 2 ? p.slots : p.gate_rows;
-  float s = 0.0f;
-  if (c < p.C)
-    for (int i = threadIdx.y; i < n; i += kSumLanes) s += src[(int64_t)i * p.C + c];
+constexpr int kSumLines = 32;
+
+__device__ __forceinline__ float sum_lines(float (*part)[33], float s, int from, int n) {  // over lines [from, from + n), in order
   part[threadIdx.y][threadIdx.x] = s;
   __syncthreads();
-  if (threadIdx.y == 0 && c < p.C) {
-    float sum = 0.0f;
+  s = 0.0f;
+  for (int i = from; i < from + n; ++i) s += part[i][threadIdx.x];
+  __syncthreads();
+  return s;
+}
+
+// Sum of lines i = first, first + stride, ... below n, eight loads at a time (one after another they took 12 us for 296 lines).
+template <class Line>
+__device__ __forceinline__ float sum_of_lines(int first, int stride, int n, Line line) {
+  float s = 0.0f;
+  for (int i = first; i < n; i += 8 * stride) {
+    float v[8];
 #pragma unroll
-    for (int i = 0; i < kSumLanes; ++i) sum += part[i][threadIdx.x];
-    dst[c] = sum;
+    for (int u = 0; u < 8; ++u) v[u] = i + u * stride < n ? *line(i + u * stride) : 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += v[u];
+  }
+  return s;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(32 * kSumLines) norm_sums_kernel(const SumParams p) {
+  using E = Element<DT>;
+  __shared__ float part[kSumLines][33];
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  const int job = p.job0 + (int)blockIdx.x % p.jobs, c = (int)(blockIdx.x / p.jobs) * 32 + threadIdx.x, line = threadIdx.y;
+  const bool on = c < p.C;
+  auto place = [&](int64_t row) { return (int)((uint64_t)row * (uint64_t)p.C & 7u); };  // of a line of sums whose first row this is
+  if (job < 2) {
+    const float* src = job == 0 ? p.pre_sums : p.post_sums;
+    if (!src) return;
+    float s = 0.0f;
+    if (on && !p.shifted) s = sum_of_lines(line, kSumLines, p.slots, [&](int i) { return src + (int64_t)i * p.pitch + c; });
+    else if (on)
+      s = sum_of_lines(line, kSumLines, p.slots, [&](int i) {
+        const int group = i / p.splits;
+        return src + (int64_t)i * p.pitch + place((int64_t)group * p.rows_per_group + (i - group * p.splits)) + c;
+      });
+    s = sum_lines(part, s, 0, kSumLines);
+    if (on && line == 0) (job == 0 ? p.d_pre_weight : p.d_post_weight)[c] = s;
+    return;
+  }
+  if (!p.unit_sums) return;
+  auto sum_of_group = [&](int64_t g, int first, int stride) {
+    return sum_of_lines(first, stride, p.gate_rows, [&](int i) {
+      return p.unit_sums + (g * p.gate_rows + i) * p.pitch + (p.shifted ? place(g * p.rows_per_group + i) : 0) + c;
+    });
+  };
+  // as many groups at a time as there are lines, or several lines for each group
+  int at_once = 1;
+  while (at_once < kSumLines && at_once < p.groups) at_once *= 2;
+  const int each = kSumLines / at_once, mine = line / each;
+  const float w = on && p.post_weight ? E::load(p.post_weight, c) : 1.0f;
+  float post = 0.0f;
+  for (int64_t g = mine; g - mine < p.groups; g += at_once) {
+    const bool here = on && g < p.groups;
+    const float gate = here && p.gate ? E::load(p.gate, g * p.C + c) : 1.0f;
+    float s = here ? sum_of_group(g, line % each, each) : 0.0f;
+    if (each > 1) s = sum_lines(part, s, mine * each, each);
+    if (here && line % each == 0) {
+      if (p.d_gate) p.d_gate[g * p.C + c] = w * s;
+      post = fmaf(gate, s, post);
+    }
+  }
+  if (p.d_post_weight && !p.post_sums) {
+    post = sum_lines(part, post, 0, kSumLines);
+    if (on && line == 0) p.d_post_weight[c] = post;
   }
 }
 
@@ -765,7 +816,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
           load_part<DT>(p.d_y, row, p.C, part, x);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] *= u[e];
-          add_sums(p.pre_sums + (int64_t)blockIdx.x * p.C, part, x, first_row);
+          add_sums(p.pre_sums + (int64_t)blockIdx.x * p.pitch, part, x, first_row);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -777,13 +828,14 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
           load_columns<DT>(p.gate, (int64_t)group * p.C, part, w);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = d[e] * v[e] * w[e];
-          add_sums(p.post_sums + (int64_t)blockIdx.x * p.C, part, x, first_row);
+          add_sums(p.post_sums + (int64_t)blockIdx.x * p.pitch, part, x, first_row);
         }
-        if (p.d_gate) {
-          load_columns<DT>(p.post_weight, 0, part, w);
+        if (p.unit_sums || p.d_gate) {
+          load_columns<DT>(p.unit_sums ? nullptr : p.post_weight, 0, part, w);
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = d[e] * v[e] * w[e];
-          add_sums(p.gate_sums ? p.gate_sums + ((int64_t)group * p.gate_rows + unit % p.splits) * p.C : p.d_gate + (int64_t)group * p.C, part, x, first_of_unit);
+          add_sums(p.unit_sums ? p.unit_sums + ((int64_t)group * p.gate_rows + unit % p.splits) * p.pitch : p.d_gate + (int64_t)group * p.C, part,
+                   x, first_of_unit);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = p.post_weight ? rstd_b * fmaf(q[e], d[e], -v[e] * mean) : q[e] * d[e];
@@ -805,8 +857,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
     const float zero[8] = {};
     for (int j = t; j < vectors; j += kWideThreads) {
       const Part none = part_of(0, p.C, j);
-      if (p.pre_sums) add_sums(p.pre_sums + (int64_t)blockIdx.x * p.C, none, zero, true);
-      if (p.post_sums) add_sums(p.post_sums + (int64_t)blockIdx.x * p.C, none, zero, true);
+      if (p.pre_sums) add_sums(p.pre_sums + (int64_t)blockIdx.x * p.pitch, none, zero, true);
+      if (p.post_sums) add_sums(p.post_sums + (int64_t)blockIdx.x * p.pitch, none, zero, true);
     }
   }
 }
@@ -827,7 +879,13 @@ struct Plan {
   int tpr, vectors, slots_per_cta, ctas, period, splits, units, gate_rows;
   bool gates;  // a slot's rows may have several gates: the kernel that carries them along
   int ids() const { return ctas * slots_per_cta; }
+  bool carries() const { return gates || tpr == 0; }  // d_post_weight needs sums of its own
+  bool by_units() const { return !carries() || splits > 1; }
+  size_t lines(int64_t groups) const {  // of sums in the workspace
+    return (size_t)ids() * (carries() ? 2 : 1) + (by_units() ? (size_t)groups * gate_rows : 0);
+  }
 };
+int64_t pitch_of(int64_t C) { return (C + 7 + 7) / 8 * 8; }  // (a row may start at the last place of its first vector)
 
 // How rows are dealt to slots (groups of threads). All rows of a slot start at the same place of a vector: they are multiples of the period
 // apart.
@@ -974,12 +1032,11 @@ size_t residual_norm_backward_floats(int64_t rows, int64_t C, int64_t groups) {
   size_t most = 0;
   for (const int64_t g : {groups, (int64_t)1}) {  // (1: a call without gates)
     for (const bool fp32 : {false, true}) {
-      const Plan plan = backward_plan(rows, C, g, fp32);
-      const size_t n = (size_t)C * (2 * (size_t)plan.ids() + (plan.splits > 1 ? (size_t)g * plan.gate_rows : 0));
-      if (n > most) most = n;
+      const size_t lines = backward_plan(rows, C, g, fp32).lines(g);
+      if (lines > most) most = lines;
     }
   }
-  return most;
+  return most * pitch_of(C);
 }
 
 cudaError_t launch_residual_norm_backward(const void* branch, const void* out, const void* d_out, const void* d_y, const void* post_weight,
@@ -989,19 +1046,26 @@ cudaError_t launch_residual_norm_backward(const void* branch, const void* out, c
                                           float* d_pre_weight, void* values, void* meta, float* workspace, cudaStream_t stream) {
   if (!gate) groups = 1;
   const Plan plan = backward_plan(rows, C, groups, dtype == SDGP_FP32);
+  const int64_t pitch = pitch_of(C), slot_floats = plan.ids() * pitch;
   float* pre_sums = d_pre_weight ? workspace : nullptr;
-  float* post_sums = d_post_weight ? workspace + (size_t)plan.ids() * C : nullptr;
-  float* gate_sums = d_gate && plan.splits > 1 ? workspace + 2 * (size_t)plan.ids() * C : nullptr;
+  float* post_sums = d_post_weight && plan.carries() ? workspace + slot_floats : nullptr;
+  float* unit_sums = plan.by_units() && (d_gate || (d_post_weight && !plan.carries())) ? workspace + slot_floats * (plan.carries() ? 2 : 1) : nullptr;
   const NormGradParams p = {branch, out, d_out, d_y, post_weight, gate, pre_weight, post_rstd, pre_rstd, d_residual, d_branch,
-                            (uint2*)values, (uint8_t*)meta, d_gate, pre_sums, post_sums, gate_sums, rows, rows / groups, (int)C,
+                            (uint2*)values, (uint8_t*)meta, d_gate, pre_sums, post_sums, unit_sums, rows, rows / groups, (int)C, (int)pitch,
                             plan.splits, plan.units, plan.gate_rows, alpha, n, m, scheme, (uint32_t)seed, (uint32_t)(seed >> 32)};
   const cudaError_t e = dtype == SDGP_BF16   ? launch_backward<SDGP_BF16>(p, plan, stream)
                         : dtype == SDGP_FP16 ? launch_backward<SDGP_FP16>(p, plan, stream)
                                              : launch_backward<SDGP_FP32>(p, plan, stream);
-  if (e != cudaSuccess || (!pre_sums && !post_sums && !gate_sums)) return e;
-  const SumParams q = {pre_sums, post_sums, gate_sums, d_pre_weight, d_post_weight, d_gate, (int)C, plan.ids(), plan.gate_rows};
-  const int64_t jobs = 2 + (gate_sums ? groups : 0);
-  return launch<norm_sums_kernel>(jobs * ((C + 31) / 32), dim3(32, kSumLanes), 0, stream, q);
+  if (e != cudaSuccess || (!pre_sums && !post_sums && !unit_sums)) return e;
+  SumParams q = {pre_sums, post_sums, unit_sums, gate, post_weight, d_pre_weight, d_post_weight, d_gate, rows / groups, groups, (int)C,
+                 (int)pitch, plan.ids(), plan.splits, plan.gate_rows, plan.tpr != 0 && plan.period != 1, 0, 0};
+  q.job0 = pre_sums ? 0 : post_sums ? 1 : 2;
+  q.jobs = (unit_sums ? 3 : post_sums ? 2 : 1) - q.job0;
+  const int64_t ctas = q.jobs * ((C + 31) / 32);
+  const dim3 block(32, kSumLines);
+  if (dtype == SDGP_BF16) return launch<norm_sums_kernel<SDGP_BF16>>(ctas, block, 0, stream, q);
+  if (dtype == SDGP_FP16) return launch<norm_sums_kernel<SDGP_FP16>>(ctas, block, 0, stream, q);
+  return launch<norm_sums_kernel<SDGP_FP32>>(ctas, block, 0, stream, q);
 }
 
 }  // namespace sdgp

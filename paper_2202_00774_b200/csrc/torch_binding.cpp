@@ -595,6 +595,12 @@ ENTRY(workspace_size_conv2d) {  // B, H, Wd, Cin, Cout, R, S, stride, pad, group
                                 : sdgp_workspace_size_conv2d(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8], flags));
 }
 
+ENTRY(workspace_size_residual_norm_backward) {  // rows, C, groups
+  Args in(args, nargs, 3);
+  const int64_t rows = in.i64(), C = in.i64(), groups = in.i64();
+  return in.ok ? PyLong_FromSize_t(sdgp_workspace_size_residual_norm_backward(rows, C, groups)) : nullptr;
+}
+
 #undef ENTRY
 
 // A C++ exception (data_ptr() of a tensor without storage, say) becomes a Python one.
@@ -612,7 +618,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 PyMethodDef methods[] = {METHOD(prune), METHOD(relu_backward_prune), METHOD(maxpool_relu_backward_prune), METHOD(dgrad_linear),
                          METHOD(dgrad_linear_static), METHOD(dgrad_conv2d), METHOD(spmm_linear), METHOD(spmm_conv2d),
                          METHOD(token_logprob), METHOD(token_logprob_backward), METHOD(residual_norm), METHOD(residual_norm_backward),
-                         METHOD(fp8_quantize), METHOD(fp8_linear),
+                         METHOD(fp8_quantize), METHOD(fp8_linear), METHOD(workspace_size_residual_norm_backward),
                          METHOD(workspace_size_linear), METHOD(workspace_size_conv2d), METHOD(linear_layer),
                          METHOD(conv2d_layer), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sdgp_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -33,7 +33,6 @@ struct Fp8Params {
   int tiles_n, tiles;  // pair kernel: feature tiles, all tiles; rows kernel: feature blocks
   int stages;
   int dtype;
-  int aligned32;    // every row of y starts on a 32-byte boundary
 };
 
 // Instruction descriptor of kind::f8f6f4: fp32 sums, e4m3 A and B (format 0), both K-major.
@@ -80,63 +79,51 @@ __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[32])
   for (int i = 16; i < 32; ++i) r[i] = 0u;
 }
 
+__device__ __forceinline__ uint64_t float_pair(float a, float b) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ void float_pair(uint64_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+// (x, y) times a pair of scales, added to a pair of sums. With single multiply-adds the pair kernel's MMAs ran a fifth slower: the warps that
+// scale share their schedulers with the thread that issues them.
+__device__ __forceinline__ void fma_pair(uint64_t& sums, uint32_t x, uint32_t y, uint64_t scale) {
+  asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}" : "+l"(sums) : "r"(x), "r"(y), "l"(scale));
+}
+
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// COLS consecutive features of one row of y, `left` of them inside it.
-template <int COLS>
-__device__ __forceinline__ void store_features(void* y, int64_t at, int64_t left, const float (&acc)[COLS], int dtype, bool aligned32) {
-  if (dtype == SDGP_FP32) {
-    float* out = (float*)y + at;
-    if (aligned32 && left >= COLS) {
-#pragma unroll
-      for (int c = 0; c < COLS; c += 8) ptx::st_global_256(out + c, (const uint32_t*)&acc[c]);
-    } else {
-#pragma unroll
-      for (int c = 0; c < COLS; ++c)
-        if (c < left) out[c] = acc[c];
-    }
-    return;
-  }
-  uint16_t* out = (uint16_t*)y + at;
-#pragma unroll
-  for (int c = 0; c < COLS; c += 16) {
-    uint32_t packed[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      packed[e] = dtype == SDGP_FP16 ? pack_pair_rn<true>(acc[c + 2 * e], acc[c + 2 * e + 1]) : pack_pair_rn<false>(acc[c + 2 * e], acc[c + 2 * e + 1]);
-    if (aligned32 && c + 16 <= left) {
-      ptx::st_global_256(out + c, packed);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (c + 2 * e < left) out[c + 2 * e] = (uint16_t)packed[e];
-        if (c + 2 * e + 1 < left) out[c + 2 * e + 1] = (uint16_t)(packed[e] >> 16);
-      }
-    }
-  }
-}
-
 // ------------------------------------------------------------------------------------------------ pairs of CTAs
 
 constexpr int kPairThreads = 384;
 constexpr int kPairMaxStages = 8;
+// Products of the two scales: of so many blocks at a time, for 128 rows and two halves of the features.
+constexpr int kScaleGroup = 4;
+constexpr int kScaleFloats = kScaleGroup * 2 * 128;
+constexpr int kStagedBytes = 8 * 4096;  // 32 rows of 128 bytes of y for each multiplying warp
+constexpr int kPairSlack = kSmemSlack + 2 * kScaleFloats * 4 + kStagedBytes;
 
 template <int BN>
 __global__ void __launch_bounds__(kPairThreads, 1)
-fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const Fp8Params p) {
+fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmY,
+                const Fp8Params p) {
   constexpr int kBufs = 512 / BN;                // accumulators in tensor memory
   constexpr int kHalf = BN / 2;                  // rows of wq that a CTA stages; features of a multiplying thread
   constexpr int kStageBytes = kTileBytes + kHalf * kBlockK;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint64_t* full = (uint64_t*)(smem + p.stages * kStageBytes);
+  uint8_t* smem = smem_raw + (-ptx::smem_u32(smem_raw) & 1023u);
+  uint8_t* staged = smem + p.stages * kStageBytes;
+  uint64_t* full = (uint64_t*)(staged + kStagedBytes);
   uint64_t* empty = full + kPairMaxStages;
   uint64_t* acc_full = empty + kPairMaxStages;
   uint64_t* acc_empty = acc_full + kBufs;
-  uint32_t* tmem_slot = (uint32_t*)(acc_empty + kBufs);
+  uint64_t* scale_full = acc_empty + kBufs;
+  uint64_t* scale_empty = scale_full + 2;
+  uint32_t* tmem_slot = (uint32_t*)(scale_empty + 2);
+  float* scales = (float*)(staged + kStagedBytes + 256);  // [2][kScaleGroup][2][128]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
   unsigned int* err = &g_device_error;
@@ -149,6 +136,10 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
     for (int a = 0; a < kBufs; ++a) {
       ptx::mbar_init(&acc_full[a], 1);
       ptx::mbar_init(&acc_empty[a], 16);  // eight warps of each CTA
+    }
+    for (int g = 0; g < 2; ++g) {
+      ptx::mbar_init(&scale_full[g], 2);
+      ptx::mbar_init(&scale_empty[g], 8);
     }
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&tmX);
@@ -210,49 +201,125 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
           }
         }
       }
+    } else if (warp >= 2) {
+      // The scales' products, four blocks at a time, into shared memory: loaded by the multiplying warps themselves - 32 lines a warp and
+      // block, from L2 since the stages leave next to no L1 - they took half of those warps' time (1130 clocks a block instead of 700).
+      const int i = threadIdx.x - 64;  // rows i and i + 64
+      int g = 0;
+      uint32_t gph = 0;
+      bool alive = true;
+      for (int t = first; alive && t < p.tiles; t += pairs) {
+        const int64_t row = (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + i, feature = (int64_t)(t % p.tiles_n) * BN;
+        const float* sx0 = p.sx + (row < p.rows ? row : 0) * p.blocks;
+        const float* sx1 = p.sx + (row + 64 < p.rows ? row + 64 : 0) * p.blocks;
+        const float* sw0 = p.sw + feature / 128 * p.blocks;
+        const float* sw1 = p.sw + (feature + kHalf < p.features ? (feature + kHalf) / 128 : 0) * p.blocks;
+        for (int b = 0; b < p.blocks; b += kScaleGroup) {
+          float x0[kScaleGroup], x1[kScaleGroup], w0[kScaleGroup], w1[kScaleGroup];
+#pragma unroll
+          for (int k = 0; k < kScaleGroup; ++k) {
+            const int at = min(b + k, p.blocks - 1);
+            x0[k] = sx0[at];
+            x1[k] = sx1[at];
+            w0[k] = sw0[at];
+            w1[k] = sw1[at];
+          }
+          if (!ptx::mbar_wait<kIdleWaitNs>(&scale_empty[g], gph ^ 1u, err, 0x900u + g)) { alive = false; break; }
+          float* to = scales + g * kScaleFloats + i;
+#pragma unroll
+          for (int k = 0; k < kScaleGroup; ++k) {
+            to[k * 256] = x0[k] * w0[k];
+            to[k * 256 + 64] = x1[k] * w0[k];
+            to[k * 256 + 128] = x0[k] * w1[k];
+            to[k * 256 + 192] = x1[k] * w1[k];
+          }
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&scale_full[g]);
+          if (++g == 2) { g = 0; gph ^= 1u; }
+        }
+      }
     }
   } else {
     more_registers<216>();
     const int half = (warp - 4) >> 2;   // which features of the tile
     const uint32_t lanes = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * kHalf);
-    int buf = 0;
-    uint32_t aph = 0;
+    const float* my_scales = scales + half * 128 + (warp & 3) * 32 + lane;
+    int buf = 0, group = 0;
+    uint32_t aph = 0, gph = 0;
     bool alive = true;
     for (int t = first; alive && t < p.tiles; t += pairs) {
       const int64_t row = (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + (warp & 3) * 32 + lane;
       const int64_t feature = (int64_t)(t % p.tiles_n) * BN + half * kHalf;
-      const float* sx = p.sx + (row < p.rows ? row : 0) * p.blocks;
-      const float* sw = p.sw + (feature < p.features ? feature / 128 : 0) * p.blocks;
-      float acc[kHalf];
+      uint64_t sums[kHalf / 2];  // pairs of features
 #pragma unroll
-      for (int c = 0; c < kHalf; ++c) acc[c] = 0.0f;
-      float next = sx[0] * sw[0];
+      for (int c = 0; c < kHalf / 2; ++c) sums[c] = 0u;
       for (int b = 0; b < p.blocks; ++b) {
-        const float scale = next;
-        if (b + 1 < p.blocks) next = sx[b + 1] * sw[b + 1];
+        const int k = b % kScaleGroup;
+        if (k == 0 && !ptx::mbar_wait(&scale_full[group], gph, err, 0xA00u + group)) { alive = false; break; }
+        const float scale = my_scales[group * kScaleFloats + k * 256];
+        const uint64_t scale2 = float_pair(scale, scale);
         if (!ptx::mbar_wait(&acc_full[buf], aph, err, 0x400u + buf)) { alive = false; break; }
         ptx::tc_fence_after_sync();
         const uint32_t from = lanes + (uint32_t)(buf * BN);
-        uint32_t v[2][32];
-        ptx::tmem_ld_32x32(from, v[0]);
+        uint32_t v[kHalf / 32][32];
 #pragma unroll
-        for (int c = 0; c < kHalf / 32; ++c) {
-          tmem_ld_wait_for(v[c & 1]);
-          if (c + 1 < kHalf / 32) {
-            ptx::tmem_ld_32x32(from + 32u * (c + 1), v[(c + 1) & 1]);
-          } else {  // all of it is in registers
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive_cluster(&acc_empty[buf], 0);
-          }
+        for (int c = 0; c < kHalf / 32; ++c) ptx::tmem_ld_32x32(from + 32u * c, v[c]);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) acc[32 * c + e] = fmaf(__uint_as_float(v[c & 1][e]), scale, acc[32 * c + e]);
+        for (int c = 0; c < kHalf / 32; ++c) tmem_ld_wait_for(v[c]);
+        ptx::tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_cluster(&acc_empty[buf], 0);
+#pragma unroll
+        for (int c = 0; c < kHalf / 32; ++c)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) fma_pair(sums[16 * c + e], v[c][2 * e], v[c][2 * e + 1], scale2);
+        if (k == kScaleGroup - 1 || b + 1 == p.blocks) {
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(&scale_empty[group]);
+          if (++group == 2) { group = 0; gph ^= 1u; }
         }
         if (++buf == kBufs) { buf = 0; aph ^= 1u; }
       }
-      if (alive && row < p.rows && feature < p.features)
-        store_features<kHalf>(p.y, row * p.features + feature, p.features - feature, acc, p.dtype, p.aligned32 != 0);
+      if (!alive) break;
+      // y through shared memory in slabs of 32 rows x 128 bytes, and by a TMA store of each (clipped at the edges): straight from the registers,
+      // 32 bytes of 32 rows at a time, a tile's stores took as long as the products of three blocks
+      float acc[kHalf];
+#pragma unroll
+      for (int c = 0; c < kHalf / 2; ++c) float_pair(sums[c], acc[2 * c], acc[2 * c + 1]);
+      uint8_t* slab = staged + (warp - 4) * 4096;
+      constexpr int kMost = kHalf / 32;  // slabs of fp32
+#pragma unroll
+      for (int c = 0; c < kMost; ++c) {
+        const bool wide = p.dtype == SDGP_FP32;
+        if (!wide && (c & 1)) continue;
+        if (lane == 0) ptx::bulk_wait_group_read<0>();  // the store before has read the slab
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          uint4 w;
+          if (wide) {
+            const int e = 32 * c + 4 * k;
+            w = make_uint4(__float_as_uint(acc[e]), __float_as_uint(acc[e + 1]), __float_as_uint(acc[e + 2]), __float_as_uint(acc[e + 3]));
+          } else {
+            const int e = (32 * c + 8 * k) % kHalf;
+            if (p.dtype == SDGP_FP16)
+              w = make_uint4(pack_pair_rn<true>(acc[e], acc[e + 1]), pack_pair_rn<true>(acc[e + 2], acc[e + 3]),
+                             pack_pair_rn<true>(acc[e + 4], acc[e + 5]), pack_pair_rn<true>(acc[e + 6], acc[e + 7]));
+            else
+              w = make_uint4(pack_pair_rn<false>(acc[e], acc[e + 1]), pack_pair_rn<false>(acc[e + 2], acc[e + 3]),
+                             pack_pair_rn<false>(acc[e + 4], acc[e + 5]), pack_pair_rn<false>(acc[e + 6], acc[e + 7]));
+          }
+          *(uint4*)(slab + lane * 128 + ((k ^ (lane & 7)) << 4)) = w;  // 128-byte swizzle
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (row < p.rows && feature + 32 * c < p.features) ptx::tma_store_2d(&tmY, slab, (int)feature + 32 * c, (int)row);
+          ptx::bulk_commit_group();
+        }
+      }
     }
+    if (lane == 0) ptx::bulk_wait_group_read<0>();
   }
   ptx::tc_fence_before_sync();
   ptx::cluster_sync();
@@ -264,21 +331,24 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
 
 constexpr int kRowsThreads = 192;
 constexpr int kRowsMaxStages = 12;
-constexpr int kRowsSlack = 1024 + 256 + 2 * 128 * 4;  // alignment, barriers, the scales of two blocks
+constexpr int kMostSplit = 8;                            // CTAs that share a sum
+constexpr int kRowsGroup = 8;                             // blocks whose scales are fetched at a time
+constexpr int kRowsSlack = 1024 + 512 + 2 * kRowsGroup * 64 * 4;  // alignment, barriers, the scales of two groups of blocks
 
 template <int T>
 __global__ void __launch_bounds__(kRowsThreads)
 fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const Fp8Params p) {
   constexpr int kStageBytes = kTileBytes + T * kBlockK;
-  constexpr uint32_t kCols = T < 16 ? 32 : 2 * T;  // two accumulators
+  constexpr int kBufs = 8;                         // accumulators: so many blocks' products may wait to be scaled
+  constexpr uint32_t kCols = kBufs * T;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* smem = smem_raw + (-ptx::smem_u32(smem_raw) & 1023u);  // (an offset: a pointer put together from integers is no longer known to be shared)
   uint64_t* full = (uint64_t*)(smem + p.stages * kStageBytes);
   uint64_t* empty = full + kRowsMaxStages;
   uint64_t* acc_full = empty + kRowsMaxStages;
-  uint64_t* acc_empty = acc_full + 2;
-  uint32_t* tmem_slot = (uint32_t*)(acc_empty + 2);
-  float* scales = (float*)(acc_empty + 4);  // [2][T]
+  uint64_t* acc_empty = acc_full + kBufs;
+  uint32_t* tmem_slot = (uint32_t*)(acc_empty + kBufs);
+  float* scales = (float*)((uint8_t*)full + 512);  // [2][kRowsGroup][T]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int split = (int)ptx::cluster_nctarank(), rank = (int)ptx::cluster_ctarank();
   unsigned int* err = &g_device_error;
@@ -288,7 +358,7 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       ptx::mbar_init(&full[s], 1);
       ptx::mbar_init(&empty[s], 1);
     }
-    for (int a = 0; a < 2; ++a) {
+    for (int a = 0; a < kBufs; ++a) {
       ptx::mbar_init(&acc_full[a], 1);
       ptx::mbar_init(&acc_empty[a], 4);
     }
@@ -311,7 +381,7 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
   const int feature_block = tile % p.tiles_n;
   const int64_t row0 = (int64_t)(tile / p.tiles_n) * T;
   const int b0 = (int)((int64_t)p.blocks * rank / split), b1 = (int)((int64_t)p.blocks * (rank + 1) / split);
-  float acc[T];  // (of the multiplying warps)
+  uint64_t sums[T / 2];  // (of the multiplying warps) pairs of rows of x
   const int f = (warp & 3) * 32 + lane;  // their feature of the block
   bool alive = true;
 
@@ -343,27 +413,42 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
         ptx::tc_commit(&empty[st]);
         ptx::tc_commit(&acc_full[buf]);
         if (++st == p.stages) { st = 0; ph ^= 1u; }
-        if (++buf == 2) { buf = 0; aph ^= 1u; }
+        if (++buf == kBufs) { buf = 0; aph ^= 1u; }
       }
     }
   } else {
     const uint32_t lanes = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-    const int i = threadIdx.x - 64;  // the row of x whose scale this thread fetches
-    const bool mine = i < T && row0 + i < p.rows;
-    const float* sx = p.sx + (mine ? row0 + i : 0) * p.blocks;
+    // the products of the two scales, eight blocks at a time, loaded while the eight before are in use: value j of a thread is row
+    // (tid + 128 j) % T of block (tid + 128 j) / T
+    constexpr int kEach = T * kRowsGroup / 128;
+    const int tid = threadIdx.x - 64;
     const float* sw = p.sw + (int64_t)feature_block * p.blocks;
+    float ahead[kEach];
+    auto load = [&](int first) {
 #pragma unroll
-    for (int c = 0; c < T; ++c) acc[c] = 0.0f;
-    float next = mine ? sx[b0] * sw[b0] : 0.0f;
+      for (int j = 0; j < kEach; ++j) {
+        const int64_t row = row0 + (tid + 128 * j) % T;
+        const int b = first + (tid + 128 * j) / T;
+        ahead[j] = row < p.rows && b < b1 ? p.sx[row * p.blocks + b] * sw[b] : 0.0f;
+      }
+    };
+#pragma unroll
+    for (int c = 0; c < T / 2; ++c) sums[c] = 0u;
+    load(b0);
     int buf = 0;
     uint32_t aph = 0;
     for (int b = b0; b < b1; ++b) {
-      if (i < T) scales[buf * T + i] = next;
-      if (mine && b + 1 < b1) next = sx[b + 1] * sw[b + 1];
-      alive = ptx::mbar_wait(&acc_full[buf], aph, err, 0x800u + buf) && alive;  // (all four warps stay in step: the barrier below)
-      ptx::named_bar_sync(1, 128);
+      const int k = (b - b0) % kRowsGroup, which = ((b - b0) / kRowsGroup) & 1;
+      if (k == 0) {
+        float* to = scales + which * kRowsGroup * T + tid;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) to[128 * j] = ahead[j];
+        load(b + kRowsGroup);
+        ptx::named_bar_sync(1, 128);  // (who writes the other group's has passed this barrier, so all have read it)
+      }
+      alive = ptx::mbar_wait(&acc_full[buf], aph, err, 0x800u + buf) && alive;  // (all four warps stay in step for that)
       ptx::tc_fence_after_sync();
-      const float* s = scales + buf * T;
+      const float* s = scales + (which * kRowsGroup + k) * T;
 #pragma unroll
       for (int c = 0; c < T; c += 32) {
         uint32_t v[32];
@@ -378,43 +463,48 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
 #pragma unroll
         for (int e = 0; e < (T < 32 ? T : 32); e += 4) {
           const float4 k = *(const float4*)(s + c + e);
-          acc[c + e] = fmaf(__uint_as_float(v[e]), k.x, acc[c + e]);
-          acc[c + e + 1] = fmaf(__uint_as_float(v[e + 1]), k.y, acc[c + e + 1]);
-          acc[c + e + 2] = fmaf(__uint_as_float(v[e + 2]), k.z, acc[c + e + 2]);
-          acc[c + e + 3] = fmaf(__uint_as_float(v[e + 3]), k.w, acc[c + e + 3]);
+          fma_pair(sums[(c + e) / 2], v[e], v[e + 1], float_pair(k.x, k.y));
+          fma_pair(sums[(c + e) / 2 + 1], v[e + 2], v[e + 3], float_pair(k.z, k.w));
         }
       }
-      buf ^= 1;
-      if (buf == 0) aph ^= 1u;
+      if (++buf == kBufs) { buf = 0; aph ^= 1u; }
     }
   }
 
   const int64_t feature = (int64_t)feature_block * 128 + f;
-  auto store = [&](int64_t row, float x) {
-    if (row >= p.rows || feature >= p.features) return;
-    const int64_t at = row * p.features + feature;
+  const int rows = (int)min((int64_t)T, p.rows - row0);
+  float acc[T];
+#pragma unroll
+  for (int c = 0; c < T / 2; ++c) float_pair(sums[c], acc[2 * c], acc[2 * c + 1]);
+  auto store = [&](int c, float x) {
+    const int64_t at = (row0 + c) * p.features + feature;
     if (p.dtype == SDGP_FP32) ((float*)p.y)[at] = x;
     else ((uint16_t*)p.y)[at] = (uint16_t)(p.dtype == SDGP_FP16 ? f32_to_f16_bits(x) : f32_to_bf16_bits(x));
   };
   if (split == 1) {
-    if (warp >= 2 && alive) {
+    if (warp >= 2 && alive && feature < p.features) {
 #pragma unroll
-      for (int c = 0; c < T; ++c) store(row0 + c, acc[c]);
+      for (int c = 0; c < T; ++c)
+        if (c < rows) store(c, acc[c]);
     }
   } else {
-    // partial sums [T][128] over the stages, which every multiplication has read to the end
+    // partial sums [T][128] over the stages, which every multiplication has read to the end; each CTA adds and stores its share of the rows of
+    // x, in the order of the CTAs
     float* partial = (float*)smem;
     if (warp >= 2) {
 #pragma unroll
       for (int c = 0; c < T; ++c) partial[c * 128 + f] = acc[c];
     }
     ptx::cluster_sync();
-    if (warp >= 2 && alive) {
-      const int c0 = T * rank / split, c1 = T * (rank + 1) / split;
-      for (int c = c0; c < c1; ++c) {
-        float sum = 0.0f;
-        for (int r = 0; r < split; ++r) sum += ptx::ld_cluster_f32(ptx::map_to_cta(&partial[c * 128 + f], (uint32_t)r));
-        store(row0 + c, sum);
+    if (warp >= 2 && alive && feature < p.features) {
+      for (int c = T * rank / split; c < min(rows, T * (rank + 1) / split); ++c) {
+        float v[kMostSplit];
+#pragma unroll
+        for (int r = 0; r < kMostSplit; ++r) v[r] = r < split ? ptx::ld_cluster_f32(ptx::map_to_cta(&partial[c * 128 + f], (uint32_t)r)) : 0.0f;
+        float sum = v[0];
+#pragma unroll
+        for (int r = 1; r < kMostSplit; ++r) sum += v[r];
+        store(c, sum);
       }
     }
     ptx::cluster_sync();
@@ -437,16 +527,22 @@ template <int BN>
 sdgp_status launch_pair(const void* xq, const void* wq, Fp8Params p, int64_t K, cudaStream_t stream) {
   static bool done[kMaxDevices] = {};
   if (!configure_once(fp8_pair_kernel<BN>, done)) return SDGP_ERR_CUDA;
-  CUtensorMap tx, tw;
+  CUtensorMap tx, tw, ty;
   if (!encode_rows(&tx, xq, p.rows, K, 128) || !encode_rows(&tw, wq, p.features, K, BN / 2)) return SDGP_ERR_CUDA;
+  // y [rows, features] in boxes of 32 rows x 128 bytes
+  const uint64_t size = p.dtype == SDGP_FP32 ? 4 : 2, dims[2] = {(uint64_t)p.features, (uint64_t)p.rows}, strides[1] = {(uint64_t)p.features * size};
+  const uint32_t box[2] = {(uint32_t)(128 / size), 32};
+  if (!encode_fresh(&ty, p.dtype == SDGP_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, p.y, dims, strides, box,
+                    CU_TENSOR_MAP_SWIZZLE_128B))
+    return SDGP_ERR_CUDA;
   constexpr int stage = kTileBytes + BN / 2 * kBlockK;
-  p.stages = (kSmemLimit - kSmemSlack) / stage;
+  p.stages = (kSmemLimit - kPairSlack) / stage;
   if (p.stages > kPairMaxStages) p.stages = kPairMaxStages;
   p.tiles_n = (int)((p.features + BN - 1) / BN);
   const int64_t tiles = (p.rows + 255) / 256 * p.tiles_n;
   if (tiles > 0x7FFFFFFF) return SDGP_ERR_UNSUPPORTED;
   p.tiles = (int)tiles;
-  return launch_pairs(fp8_pair_kernel<BN>, pairs_for(p.tiles), kPairThreads, p.stages * stage + kSmemSlack, stream, tx, tw, p);
+  return launch_pairs(fp8_pair_kernel<BN>, pairs_for(p.tiles), kPairThreads, p.stages * stage + kPairSlack, stream, tx, tw, ty, p);
 }
 
 template <int T>
@@ -460,7 +556,7 @@ sdgp_status launch_rows(const void* xq, const void* wq, Fp8Params p, int64_t K, 
   const int64_t tiles = (p.rows + T - 1) / T * p.tiles_n;
   // CTAs that share a tile's sum: as long as they are all resident at once and each has two blocks at least
   int split = 1;
-  while (split < 8 && 2 * split * tiles <= sm_count() && 4 * split <= p.blocks) split *= 2;
+  while (split < kMostSplit && 2 * split * tiles <= sm_count() && 4 * split <= p.blocks) split *= 2;
   if (tiles * split > 0x7FFFFFFF) return SDGP_ERR_UNSUPPORTED;
   p.stages = (kSmemLimit - kRowsSlack) / stage;
   if (p.stages > kRowsMaxStages) p.stages = kRowsMaxStages;
@@ -494,13 +590,13 @@ sdgp_status launch_fp8_linear(const void* xq, const float* x_scale, const void* 
   p.features = features;
   p.blocks = (int)((K + kBlockK - 1) / kBlockK);
   p.dtype = dtype;
-  p.aligned32 = (((uintptr_t)y | (uint64_t)features * (dtype == SDGP_FP32 ? 4 : 2)) & 31u) == 0;
+  // Few rows: the weights' bytes count, and the sum over K can be split. From 33 rows the pair kernel was level or ahead (4096 features, K =
+  // 4096: 33 rows 10.9 us on either, 64: 11.1 and 11.3, 256: 11.7 and 16.1, 1024: 20.5 and 58.9); its TMA stores want rows of y of
+  // whole 16 bytes.
   if (rows <= 16) return launch_rows<16>(xq, wq, p, K, stream);
   if (rows <= 32) return launch_rows<32>(xq, wq, p, K, stream);
-  if (rows <= 64) return launch_rows<64>(xq, wq, p, K, stream);
-  const int64_t pair_tiles = (rows + 255) / 256 * ((features + 255) / 256);
-  if (rows <= 128 || !p.aligned32 || pair_tiles * 4 < sm_count()) return launch_rows<128>(xq, wq, p, K, stream);
-  return launch_pair<256>(xq, wq, p, K, stream);
+  if (features * (dtype == SDGP_FP32 ? 4 : 2) % 16 != 0) return launch_rows<64>(xq, wq, p, K, stream);
+  return launch_pair<128>(xq, wq, p, K, stream);
 }
 
 }  // namespace sdgp

@@ -142,6 +142,11 @@ __device__ __forceinline__ void tma_store_5d(const void* tmap, const void* src, 
       : "memory");
 }
 
+__device__ __forceinline__ void tma_store_2d(const void* tmap, const void* src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(smem_u32(src)), "r"(c0), "r"(c1)
+               : "memory");
+}
+
 // Shared memory -> global tensor tile (TMA store), tracked by the thread's bulk async-group.
 __device__ __forceinline__ void tma_store_4d(const void* tmap, const void* src, int c0, int c1, int c2, int c3) {
   asm volatile(

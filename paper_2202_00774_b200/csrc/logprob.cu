@@ -56,12 +56,12 @@ __device__ __forceinline__ float key_value(Key k) {
 }
 
 constexpr int kMostKeys = 512;      // that a CTA collects
-constexpr int kSortAbove = 128;     // as many are sorted out: a higher bound lets fewer of what follows in
+constexpr int kSortAbove = 48;      // as many are sorted out: a higher bound lets fewer of what follows in (4096 x 131072, top 20: 329 us, 383 with 128)
 
 struct Candidates {
   Key keys[kMostKeys];
   Key best[32];
-  uint32_t bound[8];
+  uint32_t bound[16];
   int count;
 };
 
@@ -88,7 +88,7 @@ __device__ __forceinline__ void sort_out(Candidates& c, int n, int top) {
 struct LogprobParams {
   const void* logits;  // [rows, K]
   const int64_t* targets;
-  int64_t K;
+  int64_t rows, K;
   int classes;
   int top;
   float *logprob, *entropy, *lse, *top_logprob;  // entropy, lse, top_logprob, top_token: optional
@@ -101,18 +101,11 @@ constexpr int kMostParts = 8;
 // A cluster of CTAs (one where there are rows enough for all multiprocessors) reads a row in slices; its first CTA joins what the others found
 // through distributed shared memory.
 template <int DT, bool TOP, int NT>
-__global__ void __launch_bounds__(NT, NT == 32 ? 24 : 1024 / NT)
-logprob_kernel(const LogprobParams p) {
+__device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row, Stats* stats, Candidates& c) {
   using E = Element<DT>;
   constexpr int kWarps = NT / 32;
-  __shared__ Stats stats[kWarps];
-  __shared__ __align__(16) Candidates found[1];
-  Candidates& c = found[0];
-  ptx::wait_for_previous_grid();
-  ptx::launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t parts = NT == 32 ? 1u : ptx::cluster_nctarank(), part = NT == 32 ? 0u : ptx::cluster_ctarank();
-  const int64_t row = blockIdx.x / parts;
   const uint8_t* base = (const uint8_t*)p.logits + row * p.K * E::kBytes;
   // elements up to the row's first 16-byte boundary, whole vectors of eight, the rest
   const int head = min(p.classes, (int)((16u - ((uint32_t)(uintptr_t)base & 15u)) & 15u) / E::kBytes);
@@ -134,13 +127,15 @@ logprob_kernel(const LogprobParams p) {
     typename E::Raw raw[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) raw[u] = v0 + u * stride < nvec ? E::load8(body, (int64_t)(v0 + u * stride) * 8) : E::lowest8();
-    float x[kUnroll][8];
+    float x[kUnroll][8], top_of[kUnroll];
     float most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       E::widen(raw[u], x[u]);
+      top_of[u] = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) most = fmaxf(most, fmaxf(x[u][e], x[u][e + 1]));
+      for (int e = 0; e < 8; e += 2) top_of[u] = fmaxf(top_of[u], fmaxf(x[u][e], x[u][e + 1]));
+      most = fmaxf(most, top_of[u]);
     }
     {
       const float old = m;
@@ -183,6 +178,7 @@ logprob_kernel(const LogprobParams p) {
         if (most >= least) {
 #pragma unroll
           for (int u = 0; u < kUnroll; ++u) {
+            if (top_of[u] < least) continue;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               if (x[u][e] >= least && v0 + u * stride < nvec) {
@@ -260,14 +256,14 @@ logprob_kernel(const LogprobParams p) {
       for (int d = kMostParts / 2; d > 0; d >>= 1)
         st = join(st, {__shfl_xor_sync(0xFFFFFFFFu, st.m, d), __shfl_xor_sync(0xFFFFFFFFu, st.s, d), __shfl_xor_sync(0xFFFFFFFFu, st.t, d)});
       if (TOP) {
-        for (int i = threadIdx.x; i < (int)parts * 32; i += NT)
-          c.keys[i] = (i & 31) < p.top ? ptx::ld_cluster_u64(ptx::map_to_cta(&c.best[i & 31], (uint32_t)i >> 5)) : 0;
+        for (int i = threadIdx.x; i < (int)parts * p.top; i += NT)
+          c.keys[i] = ptx::ld_cluster_u64(ptx::map_to_cta(&c.best[i % p.top], (uint32_t)(i / p.top)));
         __syncthreads();
       }
     }
     ptx::cluster_sync();  // the others' shared memory has been read
     if (part != 0) return;
-    if (TOP) sort_out<NT>(c, (int)parts * 32, p.top);
+    if (TOP) sort_out<NT>(c, (int)parts * p.top, p.top);
   }
   st = {__shfl_sync(0xFFFFFFFFu, st.m, 0), __shfl_sync(0xFFFFFFFFu, st.s, 0), __shfl_sync(0xFFFFFFFFu, st.t, 0)};
   if (warp != 0) return;
@@ -286,6 +282,23 @@ logprob_kernel(const LogprobParams p) {
     const Key k = c.best[lane];
     if (p.top_token) p.top_token[row * p.top + lane] = k ? (int64_t)(uint32_t)~(uint32_t)k : -1;
     if (p.top_logprob) p.top_logprob[row * p.top + lane] = !k ? NAN : empty ? -INFINITY : (key_value(k) - st.m) - log_s;
+  }
+}
+
+template <int DT, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, NT == 32 ? 24 : 1024 / NT)
+logprob_kernel(const LogprobParams p) {
+  __shared__ Stats stats[NT / 32];
+  __shared__ __align__(16) Candidates found;
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  if constexpr (NT == 32) {  // (as many CTAs as fit; one for each row, 16384 short rows took 18 us to be dealt out)
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+      logprob_row<DT, TOP, NT>(p, row, stats, found);
+      __syncwarp();
+    }
+  } else {
+    logprob_row<DT, TOP, NT>(p, blockIdx.x / ptx::cluster_nctarank(), stats, found);
   }
 }
 
@@ -377,7 +390,7 @@ __device__ __forceinline__ void store_unit(void* dst, int64_t i, bool aligned32,
 }
 
 // Units of two vectors, all rows as one sequence of elements; a unit lies inside a row wherever K is a multiple of 16. N == 0: nothing
-// is pruned. ENTROPY: d_entropy is there.
+// is pruned. ENTROPY: d_entropy is there. For rows that are short, or of no multiple of 16 elements.
 template <int DT, int M, int N, int SCHEME, bool ENTROPY>
 __global__ void __launch_bounds__(kGradThreads)
 logprob_grad_kernel(const GradParams p) {
@@ -476,6 +489,73 @@ logprob_grad_kernel(const GradParams p) {
   }
 }
 
+// The same where rows are long and K is a multiple of 16: a CTA takes a stretch of one row, so what the row's elements share is the same for all
+// its threads and no thread has to find its row. (4096 x 131072 bf16: 15 instructions an element in the kernel above, 423 us.)
+constexpr int kStretchUnits = 4;
+constexpr int kStretch = 16 * kGradThreads * kStretchUnits;
+template <int DT, int M, int N, int SCHEME, bool ENTROPY>
+__global__ void __launch_bounds__(kGradThreads)
+logprob_grad_stretch_kernel(const GradParams p, int stretches) {
+  using E = Element<DT>;
+  ptx::wait_for_previous_grid();
+  ptx::launch_dependents();
+  const int64_t row = blockIdx.x / (unsigned)stretches;
+  const int col0 = (int)(blockIdx.x - (unsigned)row * (unsigned)stretches) * kStretch + (int)threadIdx.x * 16;
+  const int K = (int)p.K, classes = (int)p.classes;
+  const int64_t base = row * p.K;
+  typename E::Raw raw[kStretchUnits][2];
+#pragma unroll
+  for (int u = 0; u < kStretchUnits; ++u) {
+    const int col = col0 + u * 16 * kGradThreads;
+    raw[u][0].a = raw[u][0].b = raw[u][1].a = raw[u][1].b = make_uint4(0u, 0u, 0u, 0u);
+    if (col < K) load_unit<DT>(p.logits, base + col, p.aligned32, raw[u]);
+  }
+  const RowTerms r = row_terms<ENTROPY>(p, row);
+  const int64_t hot0 = r.target < p.classes ? r.target : -1;
+#pragma unroll
+  for (int u = 0; u < kStretchUnits; ++u) {
+    const int col = col0 + u * 16 * kGradThreads;
+    const bool on = col < K;
+    if (M == 32 ? !__any_sync(0xFFFFFFFFu, on) : !on) continue;
+    float x[2][8];
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      E::widen(raw[u][v], x[v]);
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float2 g = grad_of<ENTROPY>(r, {x[v][e], x[v][e + 1]});
+        x[v][e] = g.x;
+        x[v][e + 1] = g.y;
+      }
+    }
+    const int64_t hot = hot0 - col;
+    if ((uint64_t)hot < 16u) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (k == hot) x[k >> 3][k & 7] += r.hot;
+    }
+    if (r.empty || col + 16 > classes) {
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (r.empty || col + k >= classes) x[k >> 3][k & 7] = 0.0f;
+    }
+    raw[u][0] = E::narrow(x[0]);
+    raw[u][1] = E::narrow(x[1]);
+    if (on && p.grad) store_unit<DT>(p.grad, base + col, p.aligned32, raw[u]);
+    if constexpr (N > 0) {
+      const int64_t unit = (base + col) >> 4;
+      uint4 out;
+      uint32_t pa, pb;
+      KeepFlags ka, kb;
+      compress_pair<M, N, SCHEME, E::kF16>(raw[u][0].a, raw[u][1].a, 2 * unit, p.seed_lo, p.seed_hi, M == 32 ? (int)(threadIdx.x & 1) : 0,
+                                           0xFFFFFFFFu, out, pa, pb, ka, kb);
+      if (!on) continue;
+      if (p.values) p.values[unit] = out;
+      if (p.meta) p.meta[unit] = (uint16_t)prmt(pa, pb, 0x0073);
+    }
+  }
+}
+
 template <typename... Params>
 cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, int cluster, cudaStream_t stream, const Params&... args) {
   if (blocks > 0x7FFFFFFF) return cudaErrorInvalidValue;
@@ -494,22 +574,38 @@ cudaError_t launch(void (*kernel)(Params...), int64_t blocks, int threads, int c
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-constexpr int kRowThreads = 256;
 constexpr int kWarpRow = 2048;  // tokens up to which a row is one warp's
+
+template <int DT, int NT>
+cudaError_t launch_logprob_rows(const LogprobParams& p, int64_t rows, int cluster, cudaStream_t stream) {
+  return p.top > 0 ? launch(logprob_kernel<DT, true, NT>, rows * cluster, NT, cluster, stream, p)
+                   : launch(logprob_kernel<DT, false, NT>, rows * cluster, NT, cluster, stream, p);
+}
 
 template <int DT>
 cudaError_t launch_logprob_typed(const LogprobParams& p, int64_t rows, cudaStream_t stream) {
-  if (p.classes <= kWarpRow)
-    return p.top > 0 ? launch(logprob_kernel<DT, true, 32>, rows, 32, 1, stream, p) : launch(logprob_kernel<DT, false, 32>, rows, 32, 1, stream, p);
-  // CTAs that share a row: as many as it has work for, while there are too few rows to fill the multiprocessors
+  if (p.classes <= kWarpRow) {
+    const int64_t fit = 24 * (int64_t)sm_count();
+    return launch_logprob_rows<DT, 32>(p, rows < fit ? rows : fit, 1, stream);
+  }
+  // CTAs of 512 threads that share a row: as many as it has work for, while there are too few rows to fill the multiprocessors. With rows
+  // enough, CTAs of 128 threads, eight to a multiprocessor: as one's sums meet, the others read (16384 x 4096 fp32: 45 us, 84 with 256
+  // threads).
   int cluster = 1;
-  while (cluster < kMostParts && rows * cluster < 2 * (int64_t)sm_count() && p.classes > cluster * kRowThreads * 8) cluster *= 2;
-  return p.top > 0 ? launch(logprob_kernel<DT, true, kRowThreads>, rows * cluster, kRowThreads, cluster, stream, p)
-                   : launch(logprob_kernel<DT, false, kRowThreads>, rows * cluster, kRowThreads, cluster, stream, p);
+  while (cluster < kMostParts && rows * cluster < (int64_t)sm_count() && p.classes > cluster * 512 * 8) cluster *= 2;
+  if (rows <= 2 * (int64_t)sm_count()) return launch_logprob_rows<DT, 512>(p, rows, cluster, stream);
+  if (rows <= 8 * (int64_t)sm_count()) return launch_logprob_rows<DT, 256>(p, rows, 1, stream);
+  return launch_logprob_rows<DT, 128>(p, rows, 1, stream);
 }
 
 template <int DT, int M, int N, int SCHEME>
 cudaError_t launch_grad_form(const GradParams& p, int64_t blocks, cudaStream_t stream) {
+  // rows of at least half a stretch (a last stretch's idle threads end at once)
+  if (p.K % 16 == 0 && 2 * p.K >= kStretch) {
+    const int stretches = (int)((p.K + kStretch - 1) / kStretch);
+    return p.d_entropy ? launch(logprob_grad_stretch_kernel<DT, M, N, SCHEME, true>, p.rows * stretches, kGradThreads, 1, stream, p, stretches)
+                       : launch(logprob_grad_stretch_kernel<DT, M, N, SCHEME, false>, p.rows * stretches, kGradThreads, 1, stream, p, stretches);
+  }
   return p.d_entropy ? launch(logprob_grad_kernel<DT, M, N, SCHEME, true>, blocks, kGradThreads, 1, stream, p)
                      : launch(logprob_grad_kernel<DT, M, N, SCHEME, false>, blocks, kGradThreads, 1, stream, p);
 }
@@ -540,7 +636,7 @@ cudaError_t launch_grad_typed(const GradParams& p, int n, int m, int scheme, cud
 cudaError_t launch_token_logprob(const void* logits, const int64_t* targets, int64_t rows, int64_t K, int64_t classes, int dtype, int top,
                                  float* logprob, float* entropy, float* lse, float* top_logprob, int64_t* top_token,
                                  cudaStream_t stream) {
-  const LogprobParams p = {logits, targets, K, (int)classes, top, logprob, entropy, lse, top_logprob, top_token};
+  const LogprobParams p = {logits, targets, rows, K, (int)classes, top, logprob, entropy, lse, top_logprob, top_token};
   if (dtype == SDGP_BF16) return launch_logprob_typed<SDGP_BF16>(p, rows, stream);
   if (dtype == SDGP_FP16) return launch_logprob_typed<SDGP_FP16>(p, rows, stream);
   return launch_logprob_typed<SDGP_FP32>(p, rows, stream);

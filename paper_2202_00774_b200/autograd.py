@@ -167,3 +167,186 @@ def sdgp_conv2d_relu(x, weight, stride=1, padding=0, pool=False, n=2, m=4, schem
     if _plain(x):
         y = (_b._torch or _b._load()).conv2d_layer(x, weight, stride, padding, _CONV_RELU_POOL if pool else _CONV_RELU, n, m, scheme, seed)
     return _SDGPConv2dReLUFn.apply(x, weight, stride, padding, pool, n, m, scheme, seed) if y is NotImplemented else y
+
+
+# ---- a language model's layers around the pruned data gradient (Python forms only: their steps are not bound by the host) ----
+
+
+def _linear_grads(ctx, dO, vals, meta, x, weight, need_x, need_w, pattern):
+    """Input and weight gradient of ``x @ weight.T`` from the unpruned dL/dO [rows, K] and, where the pass that made it has
+    written one, its compressed pruned copy."""
+    n, m, scheme, seed = pattern
+    grad_x = grad_w = None
+    if need_x:
+        rows, K = dO.shape
+        N = weight.shape[1]
+        dt = _dtype_code(dO)
+        W = weight.contiguous()
+        dD = torch.empty((rows, N), dtype=dO.dtype, device=dO.device)
+        with torch.cuda.device(dO.device):
+            if vals is not None:
+                _b.sdgp_spmm_linear_typed(vals, meta, W, dD, dt)
+            else:
+                flags = _b.FLAG_TWO_PASS if n <= 2 or n == m else _b.FLAG_MASKED
+                ws = torch.empty(max(16, _b.sdgp_workspace_size_linear(rows, K, N, flags)), dtype=torch.uint8, device=dO.device)
+                _b.sdgp_dgrad_linear_typed(dO, W, dD, n, m, scheme, seed, dt, workspace=ws, flags=flags)
+        grad_x = dD.reshape(x.shape)
+    if need_w:
+        grad_w = dO.t() @ x.reshape(-1, x.shape[-1])   # unpruned dL/dO (Section 3.1)
+    return grad_x, grad_w
+
+
+def _compressed(rows, K, n, need_x, like):
+    """Outputs for the compressed pruned copy of dL/dO [rows, K], where the sparse contraction can take it."""
+    if n > 2 or K % 128 != 0 or not need_x:
+        return None, None
+    return (torch.empty((rows, K // 2), dtype=like.dtype, device=like.device),
+            torch.empty((rows, K // 16), dtype=torch.int16, device=like.device))
+
+
+class _SDGPLinearLogprobFn(torch.autograd.Function):
+    """The head of a language model: ``x @ weight.T`` and the log probabilities of the targets. The backward pass forms the
+    logits' gradient - the first dL/dO of the backward chain - and its compressed pruned copy in one pass."""
+
+    @staticmethod
+    def forward(ctx, x, weight, targets, classes, n, m, scheme, seed):
+        ctx.set_materialize_grads(False)
+        logits = (x @ weight.t()).reshape(-1, weight.shape[0])
+        t = targets.reshape(-1).contiguous()
+        rows = logits.shape[0]
+        logprob, entropy, lse = (torch.empty(rows, dtype=torch.float32, device=x.device) for _ in range(3))
+        _b.sdgp_token_logprob(logits, t, logprob, entropy=entropy, lse=lse, classes=classes, dtype=_dtype_code(logits))
+        ctx.save_for_backward(x, weight, logits, t, lse, entropy)
+        ctx.cfg = (classes, n, m, scheme, seed)
+        return logprob.reshape(targets.shape), entropy.reshape(targets.shape)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_logprob, d_entropy):
+        x, weight, logits, t, lse, entropy = ctx.saved_tensors
+        classes, n, m, scheme, seed = ctx.cfg
+        if d_logprob is None and d_entropy is None:
+            return (None,) * 8
+        need_x, need_w = ctx.needs_input_grad[:2]
+        flat = lambda g: None if g is None else g.reshape(-1).float().contiguous()  # noqa: E731
+        rows, K = logits.shape
+        dO = torch.empty_like(logits)
+        vals, meta = _compressed(rows, K, n, need_x, logits)
+        _b.sdgp_token_logprob_backward(logits, t, lse, flat(d_logprob), grad=dO, entropy=entropy, d_entropy=flat(d_entropy), n=n, m=m,
+                                       scheme=scheme, seed=seed, dtype=_dtype_code(logits), values=vals, meta=meta, classes=classes)
+        return (*_linear_grads(ctx, dO, vals, meta, x, weight, need_x, need_w, (n, m, scheme, seed)), None, None, None, None, None, None)
+
+
+def sdgp_linear_logprob(x, weight, targets, classes=None, n=2, m=4, scheme=_b.MAGNITUDE, seed=0):
+    """Log probabilities of ``targets`` (int64, the shape of ``x`` without its last dimension; negative: not counted, 0) under the
+    logits ``x @ weight.T``, and the entropy of every position: two float32 tensors of the shape of ``targets``. ``weight`` has one
+    row for each token; rows past ``classes`` (default: none) are padding to a multiple of 64 and get no probability. The logits'
+    gradient is formed and pruned N:M along the tokens in one pass; ``x``'s gradient is computed from the pruned copy, the weights'
+    from the unpruned one."""
+    return _SDGPLinearLogprobFn.apply(x, weight, targets, weight.shape[0] if classes is None else classes, n, m, scheme, seed)
+
+
+class _SDGPLinearResidualNormFn(torch.autograd.Function):
+    """The last layer of a block and the boundary to the next one. The backward pass writes the layer's dL/dO and its
+    compressed pruned copy in the pass that goes back through norms, gate and residual sum."""
+
+    @staticmethod
+    def forward(ctx, x, weight, residual, post_weight, pre_weight, gate, alpha, eps, n, m, scheme, seed):
+        ctx.set_materialize_grads(False)
+        branch = (x @ weight.t()).reshape(-1, weight.shape[0])
+        r = residual.reshape(branch.shape).contiguous()
+        c = lambda w: None if w is None else w.contiguous()  # noqa: E731
+        wp, wn, g = c(post_weight), c(pre_weight), c(gate)
+        f32 = dict(dtype=torch.float32, device=x.device)
+        post_rstd = torch.empty(branch.shape[0], **f32) if wp is not None else None
+        pre_rstd = torch.empty(branch.shape[0], **f32) if wn is not None else None
+        out = torch.empty_like(branch)
+        y = torch.empty_like(branch) if wn is not None else None
+        _b.sdgp_residual_norm(branch, r, out, y, post_weight=wp, gate=g, pre_weight=wn, alpha=alpha, eps=eps, dtype=_dtype_code(branch),
+                              post_rstd=post_rstd, pre_rstd=pre_rstd)
+        out = out.reshape(residual.shape)
+        y = None if y is None else y.reshape(residual.shape)
+        ctx.save_for_backward(x, weight, wp, wn, g, branch, out, post_rstd, pre_rstd)
+        ctx.cfg = (alpha, n, m, scheme, seed)
+        return out, y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, d_out, d_y):
+        x, weight, wp, wn, g, branch, out, post_rstd, pre_rstd = ctx.saved_tensors
+        alpha, n, m, scheme, seed = ctx.cfg
+        if d_out is None and d_y is None:
+            return (None,) * 12
+        need = ctx.needs_input_grad
+        flat = lambda t: None if t is None else t.reshape(branch.shape).contiguous()  # noqa: E731
+        rows, C = branch.shape
+        f32 = dict(dtype=torch.float32, device=x.device)
+        d_branch = torch.empty_like(branch) if need[0] or need[1] else None
+        d_residual = torch.empty_like(branch) if need[2] else None
+        d_post = torch.empty(C, **f32) if need[3] and wp is not None else None
+        d_pre = torch.zeros(C, **f32) if need[4] and wn is not None else None
+        d_gate = torch.empty(g.shape, **f32) if need[5] and g is not None else None
+        vals, meta = _compressed(rows, C, n, need[0], branch)
+        groups = 1 if g is None else g.numel() // C
+        ws = torch.empty(max(16, _b.sdgp_workspace_size_residual_norm_backward(rows, C, groups)), dtype=torch.uint8, device=x.device)
+        _b.sdgp_residual_norm_backward(branch, out.reshape(branch.shape), flat(d_out), flat(d_y), post_weight=wp, gate=g,
+                                       pre_weight=wn if d_y is not None else None, post_rstd=post_rstd,
+                                       pre_rstd=pre_rstd if d_y is not None else None, alpha=alpha, n=n, m=m, scheme=scheme, seed=seed,
+                                       dtype=_dtype_code(branch), d_residual=d_residual, d_branch=d_branch, d_gate=d_gate,
+                                       d_post_weight=d_post, d_pre_weight=d_pre if d_y is not None else None, values=vals, meta=meta,
+                                       workspace=ws)
+        like = lambda t, w: None if t is None else t.to(w.dtype).reshape(w.shape)  # noqa: E731
+        grad_x, grad_w = _linear_grads(ctx, d_branch, vals, meta, x, weight, need[0], need[1], (n, m, scheme, seed))
+        return (grad_x, grad_w, None if d_residual is None else d_residual.reshape(out.shape), like(d_post, wp), like(d_pre, wn),
+                like(d_gate, g), None, None, None, None, None, None)
+
+
+def sdgp_linear_residual_norm(x, weight, residual, post_weight=None, pre_weight=None, gate=None, alpha=1.0, eps=1e-6, n=2, m=4,
+                              scheme=_b.MAGNITUDE, seed=0):
+    """The last linear layer of a block with the boundary to the next block:
+    ``out = alpha * residual + gate * norm(x @ weight.T) * post_weight`` and ``y = norm(out) * pre_weight`` (root mean square norms;
+    without ``post_weight`` the branch is not normalised, without ``pre_weight`` ``y`` is None). ``gate`` has one row, one for each
+    of equal runs of positions (sequences), or one for every position. Returns ``(out, y)``. The layer's dL/dO is formed and pruned
+    N:M along its output features in one pass; gradients of weights and gate are summed in float32."""
+    return _SDGPLinearResidualNormFn.apply(x, weight, residual, post_weight, pre_weight, gate, alpha, eps, n, m, scheme, seed)
+
+
+def sdgp_fp8_weights(weight):
+    """``weight`` [out_features, in_features] in e4m3 with a scale for each 128 x 128 block, as ``sdgp_linear_fp8`` takes it: for
+    steps that use the same weights more than once."""
+    w = weight.detach().contiguous()
+    q = torch.empty(w.shape, dtype=torch.float8_e4m3fn, device=w.device)
+    scale = torch.empty((-(-w.shape[0] // 128), -(-w.shape[1] // 128)), dtype=torch.float32, device=w.device)
+    _b.sdgp_fp8_quantize(w, q, scale, block_rows=128, dtype=_b.FP32 if w.dtype == torch.float32 else _dtype_code(w))
+    return q, scale
+
+
+class _SDGPLinearFp8Fn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, wq, w_scale, n, m, scheme, seed):
+        ctx.save_for_backward(x, weight)
+        ctx.cfg = (n, m, scheme, seed)
+        rows_of_x = x.reshape(-1, x.shape[-1]).contiguous()
+        rows, K = rows_of_x.shape
+        xq = torch.empty((rows, K), dtype=torch.float8_e4m3fn, device=x.device)
+        x_scale = torch.empty((rows, -(-K // 128)), dtype=torch.float32, device=x.device)
+        _b.sdgp_fp8_quantize(rows_of_x, xq, x_scale, dtype=_dtype_code(x))
+        y = torch.empty((rows, wq.shape[0]), dtype=x.dtype, device=x.device)
+        _b.sdgp_fp8_linear(xq, x_scale, wq, w_scale, y, dtype=_dtype_code(x))
+        return y.reshape(*x.shape[:-1], wq.shape[0])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out):
+        x, weight = ctx.saved_tensors
+        dO = grad_out.reshape(-1, weight.shape[0]).contiguous()
+        return (*_linear_grads(ctx, dO, None, None, x, weight, *ctx.needs_input_grad[:2], ctx.cfg), None, None, None, None, None, None)
+
+
+def sdgp_linear_fp8(x, weight, quantized=None, n=2, m=4, scheme=_b.MAGNITUDE, seed=0):
+    """``x @ weight.T`` in 8 bits - both quantised to e4m3 with a scale for each block of 128 - whose backward pass is that of
+    ``sdgp_linear``: the roundings pass the gradient through, the input gradient is ``prune(dL/dO) @ weight`` in 16 bits, the
+    weight gradient uses the unpruned dL/dO. ``quantized``: what ``sdgp_fp8_weights(weight)`` gave. in_features and out_features
+    must be multiples of 64."""
+    wq, w_scale = sdgp_fp8_weights(weight) if quantized is None else quantized
+    return _SDGPLinearFp8Fn.apply(x, weight, wq, w_scale, n, m, scheme, seed)

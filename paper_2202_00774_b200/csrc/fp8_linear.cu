@@ -2,20 +2,22 @@
 //   y[r, f] = sum over blocks b of  sx[r, b] sw[f / 128, b]  sum over k in block b of  xq[r, k] wq[f, k]
 // the forward product of a fully connected layer (wq [features, K]), in fp32 until y is rounded.
 //
-// The scales are any fp32 numbers, so a block's sum has to be multiplied before it is added to the next one's: the tensor cores sum one block
-// of 128 into one of two accumulators in tensor memory while other warps take the other one's sums out, multiply them by the two
-// scales and add them to sums in registers. Two kernels:
+// The scales are any fp32 numbers, so a block's sum has to be multiplied before it is added to the next one's: the tensor cores sum a block
+// of 128 into one of several accumulators in tensor memory, while other warps take an earlier one's sums out, multiply them by the product of
+// the two scales and add them to sums in registers. Two kernels:
 //
-// Pairs of CTAs (fp8_pair_kernel), for many rows: a pair computes 256 rows of y and BN features; tcgen05.mma with 256 rows reads both CTAs' halves.
-// A thread of the eight multiplying warps owns one row and BN / 2 features of one weight block: both scales are numbers of that thread,
-// one fused multiply-add a sum.
-//   warp 0 TMA producer; warp 1 MMA issuer (first CTA); warps 4-11 take, scale and store.
-// What bounds it: the MMAs of a block take 512 clocks a pair (BN = 256), taking and scaling its sums about as long.
+// Pairs of CTAs (fp8_pair_kernel), for many rows: a pair computes 256 rows of y and 128 features - those of one weight block, so that a row
+// has one scale a block. tcgen05.mma with 256 rows reads both CTAs' halves of the features.
+//   warp 0 TMA producer; warp 1 MMA issuer (first CTA); warps 2, 3 products of scales; warps 4-11 take, scale and store: a thread owns one
+//   row and 64 features, two sums an instruction.
+// What bounds it: 16384 x 4096 . 4096 x 4096 takes 255 us (2.16 PFLOP/s, 64 % of twice the measured burst bf16 rate; 300 us when the chip is
+// power-limited, 66 % of twice the sustained one). With the scaling warps doing nothing but hand accumulators back, the same MMAs take 186
+// us; what they add is their instructions on the schedulers that the issuing threads share (single multiply-adds instead of pairs: 273 us).
 //
 // Features as rows of the MMA (fp8_rows_kernel), for few rows of x (one generated token for each of a batch's sequences): 128 features meet T
-// rows of x, so the weights stream through shared memory once and nothing is wasted on absent rows of x but T - rows columns. The sum is
+// rows of x, so the weights stream through shared memory once and only T - rows columns are wasted on absent rows of x. The sum over K is
 // split over a cluster of CTAs so that all multiprocessors pull weights; partial sums meet through distributed shared memory in a
-// fixed order. Bound by the weights' bytes.
+// fixed order. One row, 4096 x 4096: 5.1 us; the weights' bytes alone are 2.6.
 #include "dgrad_common.cuh"
 
 namespace sdgp {
@@ -85,8 +87,7 @@ __device__ __forceinline__ uint64_t float_pair(float a, float b) {
   return d;
 }
 __device__ __forceinline__ void float_pair(uint64_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
-// (x, y) times a pair of scales, added to a pair of sums. With single multiply-adds the pair kernel's MMAs ran a fifth slower: the warps that
-// scale share their schedulers with the thread that issues them.
+// (x, y) times a pair of scales, added to a pair of sums.
 __device__ __forceinline__ void fma_pair(uint64_t& sums, uint32_t x, uint32_t y, uint64_t scale) {
   asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}" : "+l"(sums) : "r"(x), "r"(y), "l"(scale));
 }
@@ -100,30 +101,29 @@ __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec
 
 constexpr int kPairThreads = 384;
 constexpr int kPairMaxStages = 8;
-// Products of the two scales: of so many blocks at a time, for 128 rows and two halves of the features.
-constexpr int kScaleGroup = 4;
-constexpr int kScaleFloats = kScaleGroup * 2 * 128;
+constexpr int kPairFeatures = 128;                        // features of a tile: one weight block
+constexpr int kHalf = kPairFeatures / 2;                  // rows of wq that a CTA stages; features of a scaling thread
+constexpr int kPairStage = kTileBytes + kHalf * kBlockK;
+constexpr int kPairBufs = 4;                              // accumulators
+constexpr int kScaleGroup = 4;                            // blocks whose scales are multiplied at a time
+constexpr int kScaleFloats = kScaleGroup * 128;
 constexpr int kStagedBytes = 8 * 4096;  // 32 rows of 128 bytes of y for each multiplying warp
 constexpr int kPairSlack = kSmemSlack + 2 * kScaleFloats * 4 + kStagedBytes;
 
-template <int BN>
 __global__ void __launch_bounds__(kPairThreads, 1)
 fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmY,
                 const Fp8Params p) {
-  constexpr int kBufs = 512 / BN;                // accumulators in tensor memory
-  constexpr int kHalf = BN / 2;                  // rows of wq that a CTA stages; features of a multiplying thread
-  constexpr int kStageBytes = kTileBytes + kHalf * kBlockK;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + (-ptx::smem_u32(smem_raw) & 1023u);
-  uint8_t* staged = smem + p.stages * kStageBytes;
+  uint8_t* staged = smem + p.stages * kPairStage;
   uint64_t* full = (uint64_t*)(staged + kStagedBytes);
   uint64_t* empty = full + kPairMaxStages;
   uint64_t* acc_full = empty + kPairMaxStages;
-  uint64_t* acc_empty = acc_full + kBufs;
-  uint64_t* scale_full = acc_empty + kBufs;
+  uint64_t* acc_empty = acc_full + kPairBufs;
+  uint64_t* scale_full = acc_empty + kPairBufs;
   uint64_t* scale_empty = scale_full + 2;
   uint32_t* tmem_slot = (uint32_t*)(scale_empty + 2);
-  float* scales = (float*)(staged + kStagedBytes + 256);  // [2][kScaleGroup][2][128]
+  float* scales = (float*)(staged + kStagedBytes + 256);  // [2][kScaleGroup][128]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
   unsigned int* err = &g_device_error;
@@ -133,7 +133,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       ptx::mbar_init(&full[s], 1);
       ptx::mbar_init(&empty[s], 1);
     }
-    for (int a = 0; a < kBufs; ++a) {
+    for (int a = 0; a < kPairBufs; ++a) {
       ptx::mbar_init(&acc_full[a], 1);
       ptx::mbar_init(&acc_empty[a], 16);  // eight warps of each CTA
     }
@@ -165,19 +165,19 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
         uint32_t ph = 0;
         bool alive = true;
         for (int t = first; alive && t < p.tiles; t += pairs) {
-          const int x_row = (t / p.tiles_n) * 256 + (int)rank * 128, w_row = (t % p.tiles_n) * BN + (int)rank * kHalf;
+          const int x_row = (t / p.tiles_n) * 256 + (int)rank * 128, w_row = (t % p.tiles_n) * kPairFeatures + (int)rank * kHalf;
           for (int b = 0; b < p.blocks; ++b) {
             if (!ptx::mbar_wait(&empty[st], ph ^ 1u, err, 0x100u + st)) { alive = false; break; }
-            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[st], 2u * kStageBytes);
-            ptx::tma_load_2d_pair(smem + st * kStageBytes, &tmX, &full[st], b * kBlockK, x_row);
-            ptx::tma_load_2d_pair(smem + st * kStageBytes + kTileBytes, &tmW, &full[st], b * kBlockK, w_row);
+            if (rank == 0) ptx::mbar_arrive_expect_tx(&full[st], 2u * kPairStage);
+            ptx::tma_load_2d_pair(smem + st * kPairStage, &tmX, &full[st], b * kBlockK, x_row);
+            ptx::tma_load_2d_pair(smem + st * kPairStage + kTileBytes, &tmW, &full[st], b * kBlockK, w_row);
             if (++st == p.stages) { st = 0; ph ^= 1u; }
           }
         }
       }
     } else if (warp == 1 && rank == 0) {
       if (ptx::elect_one()) {
-        constexpr uint32_t idesc = fp8_idesc(256, BN);
+        constexpr uint32_t idesc = fp8_idesc(256, kPairFeatures);
         const uint64_t desc0 = ptx::make_smem_desc(0, 16, 1024, 2);
         int st = 0, buf = 0;
         uint32_t ph = 0, aph = 0;
@@ -189,49 +189,45 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
               break;
             }
             ptx::tc_fence_after_sync();
-            const uint64_t a = desc0 + (ptx::smem_u32(smem + st * kStageBytes) >> 4);
+            const uint64_t a = desc0 + (ptx::smem_u32(smem + st * kPairStage) >> 4);
             const uint64_t w = a + (kTileBytes >> 4);
 #pragma unroll
             for (int k = 0; k < 4; ++k)  // 32 elements an instruction
-              mma_fp8_pair(tmem_base + (uint32_t)(buf * BN), a + 2 * k, w + 2 * k, idesc, k != 0);
+              mma_fp8_pair(tmem_base + (uint32_t)(buf * kPairFeatures), a + 2 * k, w + 2 * k, idesc, k != 0);
             ptx::tc_commit_pair(&empty[st], 3);
             ptx::tc_commit_pair(&acc_full[buf], 3);
             if (++st == p.stages) { st = 0; ph ^= 1u; }
-            if (++buf == kBufs) { buf = 0; aph ^= 1u; }
+            if (++buf == kPairBufs) { buf = 0; aph ^= 1u; }
           }
         }
       }
     } else if (warp >= 2) {
-      // The scales' products, four blocks at a time, into shared memory: loaded by the multiplying warps themselves - 32 lines a warp and
-      // block, from L2 since the stages leave next to no L1 - they took half of those warps' time (1130 clocks a block instead of 700).
+      // The scales' products, four blocks at a time, into shared memory. Loaded by the scaling warps themselves - 32 lines a warp and block, from
+      // L2 since the stages leave next to no L1 - they slowed the products down by a tenth.
       const int i = threadIdx.x - 64;  // rows i and i + 64
       int g = 0;
       uint32_t gph = 0;
       bool alive = true;
       for (int t = first; alive && t < p.tiles; t += pairs) {
-        const int64_t row = (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + i, feature = (int64_t)(t % p.tiles_n) * BN;
+        const int64_t row = (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + i;
         const float* sx0 = p.sx + (row < p.rows ? row : 0) * p.blocks;
         const float* sx1 = p.sx + (row + 64 < p.rows ? row + 64 : 0) * p.blocks;
-        const float* sw0 = p.sw + feature / 128 * p.blocks;
-        const float* sw1 = p.sw + (feature + kHalf < p.features ? (feature + kHalf) / 128 : 0) * p.blocks;
+        const float* sw = p.sw + (int64_t)(t % p.tiles_n) * p.blocks;
         for (int b = 0; b < p.blocks; b += kScaleGroup) {
-          float x0[kScaleGroup], x1[kScaleGroup], w0[kScaleGroup], w1[kScaleGroup];
+          float x0[kScaleGroup], x1[kScaleGroup], w[kScaleGroup];
 #pragma unroll
           for (int k = 0; k < kScaleGroup; ++k) {
             const int at = min(b + k, p.blocks - 1);
             x0[k] = sx0[at];
             x1[k] = sx1[at];
-            w0[k] = sw0[at];
-            w1[k] = sw1[at];
+            w[k] = sw[at];
           }
           if (!ptx::mbar_wait<kIdleWaitNs>(&scale_empty[g], gph ^ 1u, err, 0x900u + g)) { alive = false; break; }
           float* to = scales + g * kScaleFloats + i;
 #pragma unroll
           for (int k = 0; k < kScaleGroup; ++k) {
-            to[k * 256] = x0[k] * w0[k];
-            to[k * 256 + 64] = x1[k] * w0[k];
-            to[k * 256 + 128] = x0[k] * w1[k];
-            to[k * 256 + 192] = x1[k] * w1[k];
+            to[k * 128] = x0[k] * w[k];
+            to[k * 128 + 64] = x1[k] * w[k];
           }
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&scale_full[g]);
@@ -243,24 +239,24 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
     more_registers<216>();
     const int half = (warp - 4) >> 2;   // which features of the tile
     const uint32_t lanes = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(half * kHalf);
-    const float* my_scales = scales + half * 128 + (warp & 3) * 32 + lane;
+    const float* my_scales = scales + (warp & 3) * 32 + lane;
     int buf = 0, group = 0;
     uint32_t aph = 0, gph = 0;
     bool alive = true;
     for (int t = first; alive && t < p.tiles; t += pairs) {
       const int64_t row = (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + (warp & 3) * 32 + lane;
-      const int64_t feature = (int64_t)(t % p.tiles_n) * BN + half * kHalf;
+      const int64_t feature = (int64_t)(t % p.tiles_n) * kPairFeatures + half * kHalf;
       uint64_t sums[kHalf / 2];  // pairs of features
 #pragma unroll
       for (int c = 0; c < kHalf / 2; ++c) sums[c] = 0u;
       for (int b = 0; b < p.blocks; ++b) {
         const int k = b % kScaleGroup;
         if (k == 0 && !ptx::mbar_wait(&scale_full[group], gph, err, 0xA00u + group)) { alive = false; break; }
-        const float scale = my_scales[group * kScaleFloats + k * 256];
+        const float scale = my_scales[group * kScaleFloats + k * 128];
         const uint64_t scale2 = float_pair(scale, scale);
         if (!ptx::mbar_wait(&acc_full[buf], aph, err, 0x400u + buf)) { alive = false; break; }
         ptx::tc_fence_after_sync();
-        const uint32_t from = lanes + (uint32_t)(buf * BN);
+        const uint32_t from = lanes + (uint32_t)(buf * kPairFeatures);
         uint32_t v[kHalf / 32][32];
 #pragma unroll
         for (int c = 0; c < kHalf / 32; ++c) ptx::tmem_ld_32x32(from + 32u * c, v[c]);
@@ -278,11 +274,10 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
           if (lane == 0) ptx::mbar_arrive(&scale_empty[group]);
           if (++group == 2) { group = 0; gph ^= 1u; }
         }
-        if (++buf == kBufs) { buf = 0; aph ^= 1u; }
+        if (++buf == kPairBufs) { buf = 0; aph ^= 1u; }
       }
       if (!alive) break;
-      // y through shared memory in slabs of 32 rows x 128 bytes, and by a TMA store of each (clipped at the edges): straight from the registers,
-      // 32 bytes of 32 rows at a time, a tile's stores took as long as the products of three blocks
+      // y through shared memory, in slabs of 32 rows x 128 bytes that a TMA store each takes away (clipped at the edges)
       float acc[kHalf];
 #pragma unroll
       for (int c = 0; c < kHalf / 2; ++c) float_pair(sums[c], acc[2 * c], acc[2 * c + 1]);
@@ -333,7 +328,7 @@ constexpr int kRowsThreads = 192;
 constexpr int kRowsMaxStages = 12;
 constexpr int kMostSplit = 8;                            // CTAs that share a sum
 constexpr int kRowsGroup = 8;                             // blocks whose scales are fetched at a time
-constexpr int kRowsSlack = 1024 + 512 + 2 * kRowsGroup * 64 * 4;  // alignment, barriers, the scales of two groups of blocks
+constexpr int kRowsSlack = 1024 + 512 + 2 * kRowsGroup * 64 * 4;  // alignment, barriers, products of scales
 
 template <int T>
 __global__ void __launch_bounds__(kRowsThreads)
@@ -523,26 +518,24 @@ bool encode_rows(CUtensorMap* map, const void* base, int64_t rows, int64_t K, in
   return encode_fresh(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int BN>
 sdgp_status launch_pair(const void* xq, const void* wq, Fp8Params p, int64_t K, cudaStream_t stream) {
   static bool done[kMaxDevices] = {};
-  if (!configure_once(fp8_pair_kernel<BN>, done)) return SDGP_ERR_CUDA;
+  if (!configure_once(fp8_pair_kernel, done)) return SDGP_ERR_CUDA;
   CUtensorMap tx, tw, ty;
-  if (!encode_rows(&tx, xq, p.rows, K, 128) || !encode_rows(&tw, wq, p.features, K, BN / 2)) return SDGP_ERR_CUDA;
+  if (!encode_rows(&tx, xq, p.rows, K, 128) || !encode_rows(&tw, wq, p.features, K, kHalf)) return SDGP_ERR_CUDA;
   // y [rows, features] in boxes of 32 rows x 128 bytes
   const uint64_t size = p.dtype == SDGP_FP32 ? 4 : 2, dims[2] = {(uint64_t)p.features, (uint64_t)p.rows}, strides[1] = {(uint64_t)p.features * size};
   const uint32_t box[2] = {(uint32_t)(128 / size), 32};
   if (!encode_fresh(&ty, p.dtype == SDGP_FP32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, p.y, dims, strides, box,
                     CU_TENSOR_MAP_SWIZZLE_128B))
     return SDGP_ERR_CUDA;
-  constexpr int stage = kTileBytes + BN / 2 * kBlockK;
-  p.stages = (kSmemLimit - kPairSlack) / stage;
+  p.stages = (kSmemLimit - kPairSlack) / kPairStage;
   if (p.stages > kPairMaxStages) p.stages = kPairMaxStages;
-  p.tiles_n = (int)((p.features + BN - 1) / BN);
+  p.tiles_n = (int)((p.features + kPairFeatures - 1) / kPairFeatures);
   const int64_t tiles = (p.rows + 255) / 256 * p.tiles_n;
   if (tiles > 0x7FFFFFFF) return SDGP_ERR_UNSUPPORTED;
   p.tiles = (int)tiles;
-  return launch_pairs(fp8_pair_kernel<BN>, pairs_for(p.tiles), kPairThreads, p.stages * stage + kPairSlack, stream, tx, tw, ty, p);
+  return launch_pairs(fp8_pair_kernel, pairs_for(p.tiles), kPairThreads, p.stages * kPairStage + kPairSlack, stream, tx, tw, ty, p);
 }
 
 template <int T>
@@ -596,7 +589,7 @@ sdgp_status launch_fp8_linear(const void* xq, const float* x_scale, const void* 
   if (rows <= 16) return launch_rows<16>(xq, wq, p, K, stream);
   if (rows <= 32) return launch_rows<32>(xq, wq, p, K, stream);
   if (features * (dtype == SDGP_FP32 ? 4 : 2) % 16 != 0) return launch_rows<64>(xq, wq, p, K, stream);
-  return launch_pair<128>(xq, wq, p, K, stream);
+  return launch_pair(xq, wq, p, K, stream);
 }
 
 }  // namespace sdgp

@@ -500,13 +500,14 @@ logprob_grad_stretch_kernel(const GradParams p, int stretches) {
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
   const int64_t row = blockIdx.x / (unsigned)stretches;
-  const int col0 = (int)(blockIdx.x - (unsigned)row * (unsigned)stretches) * kStretch + (int)threadIdx.x * 16;
-  const int K = (int)p.K, classes = (int)p.classes;
+  // (unsigned: the last stretch of a row may end past 2^31)
+  const uint32_t col0 = (blockIdx.x - (uint32_t)row * (uint32_t)stretches) * kStretch + threadIdx.x * 16;
+  const uint32_t K = (uint32_t)p.K, classes = (uint32_t)p.classes;
   const int64_t base = row * p.K;
   typename E::Raw raw[kStretchUnits][2];
 #pragma unroll
   for (int u = 0; u < kStretchUnits; ++u) {
-    const int col = col0 + u * 16 * kGradThreads;
+    const uint32_t col = col0 + u * 16 * kGradThreads;
     raw[u][0].a = raw[u][0].b = raw[u][1].a = raw[u][1].b = make_uint4(0u, 0u, 0u, 0u);
     if (col < K) load_unit<DT>(p.logits, base + col, p.aligned32, raw[u]);
   }
@@ -514,7 +515,7 @@ logprob_grad_stretch_kernel(const GradParams p, int stretches) {
   const int64_t hot0 = r.target < p.classes ? r.target : -1;
 #pragma unroll
   for (int u = 0; u < kStretchUnits; ++u) {
-    const int col = col0 + u * 16 * kGradThreads;
+    const uint32_t col = col0 + u * 16 * kGradThreads;
     const bool on = col < K;
     if (M == 32 ? !__any_sync(0xFFFFFFFFu, on) : !on) continue;
     float x[2][8];
@@ -528,7 +529,7 @@ logprob_grad_stretch_kernel(const GradParams p, int stretches) {
         x[v][e + 1] = g.y;
       }
     }
-    const int64_t hot = hot0 - col;
+    const int64_t hot = hot0 - (int64_t)col;
     if ((uint64_t)hot < 16u) {
 #pragma unroll
       for (int k = 0; k < 16; ++k)

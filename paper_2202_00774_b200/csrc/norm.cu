@@ -159,11 +159,12 @@ struct NormParams {
   float alpha, eps;
 };
 
-template <int DT, int TPR>
+// A thread owns NV vectors, TPR apart.
+template <int DT, int TPR, int NV>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 512 ? 1 : 1024 / kCtaThreads<TPR>)
 norm_kernel(const NormParams p) {
   using E = Element<DT>;
-  using R = Ring<DT, TPR, 2, 1>;
+  using R = Ring<DT, TPR, 2 * NV, 1>;
   constexpr int SLOTS = kCtaThreads<TPR> / TPR;
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ float buffer[2 * SLOTS * kMaxWarpsPerRow];
@@ -172,54 +173,79 @@ norm_kernel(const NormParams p) {
   const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR;
   const int64_t first = (int64_t)blockIdx.x * SLOTS + slot, stride = (int64_t)gridDim.x * SLOTS;
   if (first >= p.rows) return;  // (a slot's threads share no barrier with the others)
-  const Part part = part_of(first, p.C, t);
+  Part part[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) part[j] = part_of(first, p.C, t + j * TPR);
   uint8_t* mine = ring + threadIdx.x * 16;
   const uint32_t mine_u32 = ptx::smem_u32(mine);
   auto fetch = [&](int64_t row, int stage) {
     if (row < p.rows) {
-      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage, p.branch, row * p.C, part);
-      copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + R::kVec, p.residual, row * p.C, part);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + 2 * j * R::kVec, p.branch, row * p.C, part[j]);
+        copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + (2 * j + 1) * R::kVec, p.residual, row * p.C, part[j]);
+      }
     }
     cp_async_commit();
   };
 #pragma unroll
   for (int s = 0; s < R::kStages; ++s) fetch(first + s * stride, s);
-  const typename E::Raw w_post = column_part<DT>(p.post_weight, 0, part), w_pre = column_part<DT>(p.pre_weight, 0, part);
-  typename E::Raw gate = column_part<DT>(p.gate, 0, part);
+  typename E::Raw w_post[NV], w_pre[NV], gate[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    w_post[j] = column_part<DT>(p.post_weight, 0, part[j]);
+    w_pre[j] = column_part<DT>(p.pre_weight, 0, part[j]);
+    gate[j] = column_part<DT>(p.gate, 0, part[j]);
+  }
   const float inv_c = 1.0f / (float)p.C;
   int stage = 0, turn = 0;
   for (int64_t row = first; row < p.rows; row += stride) {
-    if (p.groups > 1) gate = column_part<DT>(p.gate, row / p.rows_per_group * p.C, part);
-    cp_async_wait<R::kStages - 1>();
-    float b[8], r[8], w[8], g[8];
-    read_part<DT, R::kChunk, false>(mine + stage * R::kStage, part, b);
-    read_part<DT, R::kChunk, false>(mine + stage * R::kStage + R::kVec, part, r);
-    E::widen(gate, g);
-    if (p.post_weight) {
-      float s[1] = {0.0f};
+    if (p.groups > 1) {
+      const int64_t at = row / p.rows_per_group * p.C;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] = fmaf(b[e], b[e], s[0]);
-      row_sums<TPR>(s, buffer, slot, turn);
-      const float rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
-      if (t == 0 && p.post_rstd) p.post_rstd[row] = rstd;
-      E::widen(w_post, w);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) b[e] = b[e] * rstd * w[e];
+      for (int j = 0; j < NV; ++j) gate[j] = column_part<DT>(p.gate, at, part[j]);
     }
+    cp_async_wait<R::kStages - 1>();
+    float o[NV][8], rstd = 1.0f;  // the branch, then its sum with the residual
+    float s[1] = {0.0f};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = fmaf(g[e], b[e], p.alpha * r[e]);
-    write_part<DT>(p.out, row * p.C, part, E::narrow(r), r);
-    if (p.pre_weight) {  // (of the sums before their rounding to 16 bits)
-      float s[1] = {0.0f};
+    for (int j = 0; j < NV; ++j) {
+      read_part<DT, R::kChunk, false>(mine + stage * R::kStage + 2 * j * R::kVec, part[j], o[j]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] = fmaf(r[e], r[e], s[0]);
+      for (int e = 0; e < 8; ++e) s[0] = fmaf(o[j][e], o[j][e], s[0]);
+    }
+    if (p.post_weight) {
       row_sums<TPR>(s, buffer, slot, turn);
-      const float rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
-      if (t == 0 && p.pre_rstd) p.pre_rstd[row] = rstd;
-      E::widen(w_pre, w);
+      rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
+      if (t == 0 && p.post_rstd) p.post_rstd[row] = rstd;
+    }
+    s[0] = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) r[e] = r[e] * rstd * w[e];
-      write_part<DT>(p.y, row * p.C, part, E::narrow(r), r);
+    for (int j = 0; j < NV; ++j) {
+      float r[8], w[8], g[8];
+      read_part<DT, R::kChunk, false>(mine + stage * R::kStage + (2 * j + 1) * R::kVec, part[j], r);
+      E::widen(w_post[j], w);
+      E::widen(gate[j], g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float n = p.post_weight ? o[j][e] * rstd * w[e] : o[j][e];
+        o[j][e] = fmaf(g[e], n, p.alpha * r[e]);
+        s[0] = fmaf(o[j][e], o[j][e], s[0]);
+      }
+      write_part<DT>(p.out, row * p.C, part[j], E::narrow(o[j]), o[j]);
+    }
+    if (p.pre_weight) {  // (of the sums before their rounding to 16 bits)
+      row_sums<TPR>(s, buffer, slot, turn);
+      rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
+      if (t == 0 && p.pre_rstd) p.pre_rstd[row] = rstd;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float w[8];
+        E::widen(w_pre[j], w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[j][e] = o[j][e] * rstd * w[e];
+        write_part<DT>(p.y, row * p.C, part[j], E::narrow(o[j]), o[j]);
+      }
     }
     fetch(row + R::kStages * stride, stage);
     if (++stage == R::kStages) stage = 0;
@@ -326,18 +352,21 @@ __device__ __forceinline__ float warp_sums3(float a, float b, float c) {
 //
 // GATES: a slot's rows have more than one gate, so gates go along with the rows. Else q = g w_post stays in registers, and a thread has
 // room for NV = 2 vectors, TPR threads apart: half the exchanges, addresses and barriers an element.
-template <int DT, int TPR, int NV, bool GATES, bool ALIGNED, bool PRUNE>
+// CL: CTAs that share rows too wide for one; each writes its warps' sums to all, and a cluster barrier takes the barrier's place.
+template <int DT, int TPR, int NV, int CL, bool GATES, bool ALIGNED, bool PRUNE>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 256 ? 1 : 2)
 norm_grad_kernel(const NormGradParams p) {
   using E = Element<DT>;
   using R = Ring<DT, TPR, 4 * NV, 2>;
-  constexpr int SLOTS = kCtaThreads<TPR> / TPR, S = R::kStages, W = TPR / 32;
+  constexpr int SLOTS = kCtaThreads<TPR> / TPR, S = R::kStages, W = TPR / 32, WC = W * CL;  // WC: warps of a row
+  static_assert(CL == 1 || SLOTS == 1, "");
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float buffer[2 * 3 * SLOTS * W];
+  __shared__ float buffer[2 * 3 * SLOTS * WC];
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
   const int slot = threadIdx.x / TPR, t = threadIdx.x % TPR, lane = threadIdx.x & 31;
-  const int id = (int)blockIdx.x * SLOTS + slot, ids = (int)gridDim.x * SLOTS;
+  const int rank = CL > 1 ? (int)ptx::cluster_ctarank() : 0, v0 = rank * TPR * NV + t;  // v0: the thread's first vector of a row
+  const int id = (int)blockIdx.x / CL * SLOTS + slot, ids = (int)gridDim.x / CL * SLOTS;
   const int64_t step = (int64_t)p.splits * p.C;
   Walk here;
   here.unit = id;
@@ -347,7 +376,7 @@ norm_grad_kernel(const NormGradParams p) {
     const float2 zero[4] = {};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int at = (t + j * TPR) * 8;
+      const int at = (v0 + j * TPR) * 8;
       if (at < p.pitch && p.pre_sums) write_sums(p.pre_sums + (int64_t)id * p.pitch + at, zero);
       if (at < p.pitch && p.post_sums) write_sums(p.post_sums + (int64_t)id * p.pitch + at, zero);
     }
@@ -355,7 +384,7 @@ norm_grad_kernel(const NormGradParams p) {
   }
   Part part[NV];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) part[j] = part_of(here.row, p.C, t + j * TPR);
+  for (int j = 0; j < NV; ++j) part[j] = part_of(here.row, p.C, v0 + j * TPR);
   uint8_t* mine = ring + threadIdx.x * 16;
   const uint32_t mine_u32 = ptx::smem_u32(mine);
   auto fetch = [&](const Walk& w, int stage) {
@@ -398,6 +427,11 @@ norm_grad_kernel(const NormGradParams p) {
       for (int e = 0; e < 8; ++e) q[e] = q_kept[j][e];
     }
   };
+  auto meet = [&]() {
+    if (CL > 1) ptx::cluster_sync();
+    else if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
+  };
+  if (CL > 1) ptx::cluster_sync();  // the others run: their shared memory may be written
   const float inv_c = 1.0f / (float)p.C;
   auto sum_row = [&](const Beside& beside, int stage, int turn) -> float {
     float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
@@ -420,7 +454,15 @@ norm_grad_kernel(const NormGradParams p) {
       }
     }
     const float s = warp_sums3(beside.rstd * (s0.x + s0.y), beside.rstd_b * (s1.x + s1.y), beside.rstd_b * beside.rstd * (s2.x + s2.y));
-    if (TPR > 32 && (lane & 7) == 0 && lane != 24) buffer[(turn * SLOTS + slot) * W * 3 + (lane == 0 ? 0 : lane == 16 ? W : 2 * W) + (t >> 5)] = s;
+    if (TPR > 32 && (lane & 7) == 0 && lane != 24) {
+      float* to = &buffer[(turn * SLOTS + slot) * WC * 3 + (lane == 0 ? 0 : lane == 16 ? WC : 2 * WC) + rank * W + (t >> 5)];
+      if constexpr (CL == 1) {
+        *to = s;
+      } else {
+#pragma unroll
+        for (int c = 0; c < CL; ++c) ptx::st_cluster_f32(ptx::map_to_cta(to, (uint32_t)c), s);
+      }
+    }
     return s;
   };
 
@@ -464,7 +506,7 @@ norm_grad_kernel(const NormGradParams p) {
   }
   cp_async_wait<S - 1>();
   float own = sum_row(beside, 0, 0), own_next = own;
-  if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
+  meet();
 
   float2 pre_sum[NV][4] = {}, post_sum[NV][4] = {}, gate_sum[NV][4] = {};
   int stage = 0, turn = 0;
@@ -477,10 +519,17 @@ norm_grad_kernel(const NormGradParams p) {
     }
     float s0, s1, s2;
     if constexpr (TPR > 32) {
-      const float* from = buffer + (turn * SLOTS + slot) * W * 3 + lane % W;
-      s0 = sum_lanes<W>(from[0]);
-      s1 = sum_lanes<W>(from[W]);
-      s2 = sum_lanes<W>(from[2 * W]);
+      constexpr int L = WC < 32 ? WC : 32;
+      const float* from = buffer + (turn * SLOTS + slot) * WC * 3 + lane % L;
+      s0 = from[0], s1 = from[WC], s2 = from[2 * WC];
+      if constexpr (WC > 32) {
+        s0 += from[32];
+        s1 += from[WC + 32];
+        s2 += from[2 * WC + 32];
+      }
+      s0 = sum_lanes<L>(s0);
+      s1 = sum_lanes<L>(s1);
+      s2 = sum_lanes<L>(s2);
     } else {
       s0 = __shfl_sync(0xFFFFFFFFu, own, 0);
       s1 = __shfl_sync(0xFFFFFFFFu, own, 16);
@@ -527,7 +576,7 @@ norm_grad_kernel(const NormGradParams p) {
       const typename E::Raw packed = E::narrow(out);
       if (p.d_branch) write_part<DT, ALIGNED>(p.d_branch, here.at, part[j], packed, out);
       if constexpr (PRUNE) {  // (rows of whole groups of 16: every part is full or empty, and a group's lanes alike)
-        const int64_t vec = (here.at >> 3) + t + j * TPR;
+        const int64_t vec = (here.at >> 3) + v0 + j * TPR;
         const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, t & 3);
         if (part[j].full) {
           if (p.values) p.values[vec] = make_uint2(c.x, c.y);
@@ -537,7 +586,7 @@ norm_grad_kernel(const NormGradParams p) {
       if (unit_ends) {  // sum of d v over the unit's rows: times g for d_w_post, times w_post for d_g
         const bool some = part[j].hi > 0;
         if (p.unit_sums && some)
-          write_sums(p.unit_sums + ((int64_t)here.group * p.gate_rows + (here.unit - here.group * p.splits)) * p.pitch + (t + j * TPR) * 8, gate_sum[j]);
+          write_sums(p.unit_sums + ((int64_t)here.group * p.gate_rows + (here.unit - here.group * p.splits)) * p.pitch + (v0 + j * TPR) * 8, gate_sum[j]);
         if constexpr (GATES) {
           float g[8], w[8];
           E::widen(beside.gate, g);
@@ -563,13 +612,13 @@ norm_grad_kernel(const NormGradParams p) {
     own = own_next;
     stage = stage_next;
     turn ^= 1;
-    if (TPR > 32) ptx::named_bar_sync(1 + slot, TPR);
+    meet();
   }
   cp_async_wait<0>();
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     if (part[j].hi <= 0) continue;
-    const int64_t at = (int64_t)id * p.pitch + (t + j * TPR) * 8;
+    const int64_t at = (int64_t)id * p.pitch + (v0 + j * TPR) * 8;
     if (p.pre_sums) write_sums(p.pre_sums + at, pre_sum[j]);
     if (GATES && p.post_sums) write_sums(p.post_sums + at, post_sum[j]);
   }
@@ -876,7 +925,7 @@ int threads_of_row(int64_t C, int vectors, int most) {
 }
 
 struct Plan {
-  int tpr, vectors, slots_per_cta, ctas, period, splits, units, gate_rows;
+  int tpr, vectors, cluster, slots_per_cta, ctas, period, splits, units, gate_rows;  // ctas: clusters of them where cluster > 1
   bool gates;  // a slot's rows may have several gates: the kernel that carries them along
   int ids() const { return ctas * slots_per_cta; }
   bool carries() const { return gates || tpr == 0; }  // d_post_weight needs sums of its own
@@ -892,7 +941,7 @@ int64_t pitch_of(int64_t C) { return (C + 7 + 7) / 8 * 8; }  // (a row may start
 Plan plan_slots(int64_t rows, int64_t C, int tpr, int ctas_per_sm) {
   Plan p = {};
   p.tpr = tpr;
-  p.vectors = 1;
+  p.vectors = p.cluster = 1;
   p.slots_per_cta = tpr == 0 || tpr >= 256 ? 1 : 256 / tpr;
   p.period = 8 / gcd8((int)(C % 8));
   const int64_t most = (int64_t)sm_count() * ctas_per_sm, wanted = (rows + p.slots_per_cta - 1) / p.slots_per_cta;
@@ -902,8 +951,10 @@ Plan plan_slots(int64_t rows, int64_t C, int tpr, int ctas_per_sm) {
 
 // Forward: rows at the stride of all slots.
 Plan forward_plan(int64_t rows, int64_t C) {
-  const int tpr = threads_of_row(C, 1, 1024);
+  int tpr = threads_of_row(C, 1, 1024), vectors = 1;
+  if (tpr == 0) tpr = threads_of_row(C, vectors = 2, 1024);
   Plan p = plan_slots(rows, C, tpr, tpr == 0 ? 2 : tpr > 512 ? 1 : tpr > 256 ? 2 : 4);
+  p.vectors = vectors;
   if (p.ids() < rows && p.period > p.slots_per_cta) p.ctas -= p.ctas % (p.period / p.slots_per_cta);
   return p;
 }
@@ -937,10 +988,17 @@ Plan deal_units(Plan p, int64_t rows, int64_t groups) {
 Plan backward_plan(int64_t rows, int64_t C, int64_t groups, bool fp32) {
   // one gate a slot: two vectors a thread (fp32: shared memory holds the stages of one)
   const int vectors = fp32 ? 1 : 2;
-  int tpr = threads_of_row(C, vectors, 512);
+  int tpr = 0, cluster = 1;
+  for (; tpr == 0 && cluster <= 4; cluster *= 2) tpr = threads_of_row(C, vectors * cluster, 512);
+  cluster /= 2;
   if (tpr != 0) {
-    Plan p = deal_units(plan_slots(rows, C, tpr, tpr > 256 ? 1 : 2), rows, groups);
+    Plan p = plan_slots(rows, C, tpr, tpr > 256 ? 1 : 2);
+    // (clusters of four: not every multiprocessor finds three neighbours)
+    const int fit = cluster == 4 ? sm_count() / 4 * 7 / 8 : sm_count() / 2;
+    if (cluster > 1 && p.ctas > fit) p.ctas = fit;
+    p = deal_units(p, rows, groups);
     p.vectors = vectors;
+    p.cluster = cluster;
     if (!p.gates) return p;
   }
   tpr = threads_of_row(C, 1, fp32 ? 512 : 1024);
@@ -950,7 +1008,7 @@ Plan backward_plan(int64_t rows, int64_t C, int64_t groups, bool fp32) {
 }
 
 template <auto Kernel, typename... Args>
-cudaError_t launch(int64_t ctas, dim3 block, int smem, cudaStream_t stream, const Args&... args) {
+cudaError_t launch(int64_t ctas, dim3 block, int smem, int cluster, cudaStream_t stream, const Args&... args) {
   static bool done[kMaxDevices] = {};  // (what a kernel asks for is always the same)
   const int dev = current_device();
   if (dev < 0) return cudaErrorInvalidDevice;
@@ -965,45 +1023,52 @@ cudaError_t launch(int64_t ctas, dim3 block, int smem, cudaStream_t stream, cons
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, Kernel, args...);
 }
 
 template <int DT>
 cudaError_t launch_forward(const NormParams& p, const Plan& plan, cudaStream_t stream) {
-  switch (plan.tpr) {
-#define SDGP_ROW(T) \
-  case T: return launch<norm_kernel<DT, T>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 2, 1>::kBytes, stream, p);
-    SDGP_ROW(32) SDGP_ROW(64) SDGP_ROW(128) SDGP_ROW(256) SDGP_ROW(512) SDGP_ROW(1024)
+  switch (plan.tpr * plan.vectors) {
+#define SDGP_ROW(T, NV) \
+  case T * NV: return launch<norm_kernel<DT, T, NV>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 2 * NV, 1>::kBytes, 1, stream, p);
+    SDGP_ROW(32, 1) SDGP_ROW(64, 1) SDGP_ROW(128, 1) SDGP_ROW(256, 1) SDGP_ROW(512, 1) SDGP_ROW(1024, 1) SDGP_ROW(1024, 2)
 #undef SDGP_ROW
   }
-  return launch<norm_wide_kernel<DT>>(plan.ctas, dim3(kWideThreads), 0, stream, p);
+  return launch<norm_wide_kernel<DT>>(plan.ctas, dim3(kWideThreads), 0, 1, stream, p);
 }
 
 template <int DT, bool ALIGNED, bool PRUNE>
 cudaError_t launch_backward_form(const NormGradParams& p, const Plan& plan, cudaStream_t stream) {
-#define SDGP_ROW(T, NV, GATES)                                                                                                      \
-  case T: return launch<norm_grad_kernel<DT, T, NV, GATES, ALIGNED, PRUNE>>(plan.ctas, dim3(kCtaThreads<T>), Ring<DT, T, 4 * NV, 2>::kBytes, \
-                                                                             stream, p);
+#define SDGP_ROW(T, NV, CL, GATES)                                                                                                \
+  case T * CL:                                                                                                                     \
+    return launch<norm_grad_kernel<DT, T, NV, CL, GATES, ALIGNED, PRUNE>>((int64_t)plan.ctas * CL, dim3(kCtaThreads<T>),            \
+                                                                          Ring<DT, T, 4 * NV, 2>::kBytes, CL, stream, p);
   if (!plan.gates) {
     constexpr int NV = DT == SDGP_FP32 ? 1 : 2;
     if (plan.vectors == NV) {
-      switch (plan.tpr) { SDGP_ROW(32, NV, false) SDGP_ROW(64, NV, false) SDGP_ROW(128, NV, false) SDGP_ROW(256, NV, false) SDGP_ROW(512, NV, false) }
+      switch (plan.tpr * plan.cluster) {
+        SDGP_ROW(32, NV, 1, false) SDGP_ROW(64, NV, 1, false) SDGP_ROW(128, NV, 1, false) SDGP_ROW(256, NV, 1, false) SDGP_ROW(512, NV, 1, false)
+        SDGP_ROW(512, NV, 2, false) SDGP_ROW(512, NV, 4, false)
+      }
     }
   } else {
     switch (plan.tpr) {
-      SDGP_ROW(32, 1, true) SDGP_ROW(64, 1, true) SDGP_ROW(128, 1, true) SDGP_ROW(256, 1, true) SDGP_ROW(512, 1, true)
+      SDGP_ROW(32, 1, 1, true) SDGP_ROW(64, 1, 1, true) SDGP_ROW(128, 1, 1, true) SDGP_ROW(256, 1, 1, true) SDGP_ROW(512, 1, 1, true)
     }
     if constexpr (DT != SDGP_FP32) {
-      switch (plan.tpr) { SDGP_ROW(1024, 1, true) }
+      switch (plan.tpr) { SDGP_ROW(1024, 1, 1, true) }
     }
   }
 #undef SDGP_ROW
-  return launch<norm_grad_wide_kernel<DT, PRUNE>>(plan.ctas, dim3(kWideThreads), 0, stream, p);
+  return launch<norm_grad_wide_kernel<DT, PRUNE>>(plan.ctas, dim3(kWideThreads), 0, 1, stream, p);
 }
 
 template <int DT>
@@ -1063,9 +1128,9 @@ cudaError_t launch_residual_norm_backward(const void* branch, const void* out, c
   q.jobs = (unit_sums ? 3 : post_sums ? 2 : 1) - q.job0;
   const int64_t ctas = q.jobs * ((C + 31) / 32);
   const dim3 block(32, kSumLines);
-  if (dtype == SDGP_BF16) return launch<norm_sums_kernel<SDGP_BF16>>(ctas, block, 0, stream, q);
-  if (dtype == SDGP_FP16) return launch<norm_sums_kernel<SDGP_FP16>>(ctas, block, 0, stream, q);
-  return launch<norm_sums_kernel<SDGP_FP32>>(ctas, block, 0, stream, q);
+  if (dtype == SDGP_BF16) return launch<norm_sums_kernel<SDGP_BF16>>(ctas, block, 0, 1, stream, q);
+  if (dtype == SDGP_FP16) return launch<norm_sums_kernel<SDGP_FP16>>(ctas, block, 0, 1, stream, q);
+  return launch<norm_sums_kernel<SDGP_FP32>>(ctas, block, 0, 1, stream, q);
 }
 
 }  // namespace sdgp

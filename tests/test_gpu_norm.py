@@ -120,7 +120,8 @@ def near(x, want, size, dtype, n):
 
 SHAPES = [(1, 1, 1), (2, 3, 1), (5, 8, 5), (7, 17, 1), (3, 64, 1), (33, 250, 1), (130, 256, 2), (64, 263, 8), (40, 1024, 40), (700, 520, 7),
           (19, 1999, 1), (24, 1999, 8), (1064, 1001, 8), (300, 2044, 300), (9, 4096, 1), (500, 4096, 2), (3, 8185, 3), (4, 8192, 1), (6, 8193, 2),
-          (5, 16384, 1), (300, 12002, 3), (21, 1003, 7), (600, 99, 200), (2000, 36, 500), (3000, 40, 3000), (4001, 51, 4001)]
+          (5, 16384, 1), (300, 12002, 3), (21, 1003, 7), (600, 99, 200), (2000, 36, 500), (3000, 40, 3000), (4001, 51, 4001),
+          (300, 16383, 1), (7, 20000, 1), (200, 24000, 2), (40, 32761, 1), (9, 40000, 3)]
 
 
 @pytest.mark.parametrize("dtype", [B.BF16, B.FP16, B.FP32])

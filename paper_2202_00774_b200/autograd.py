@@ -2,13 +2,14 @@
 and computes the input gradient with the SDGP kernels (Algorithm 1; Section 3.1: "SDGP only
 changes the data gradient; the weight gradient uses the unpruned dL/dO").
 
-Only the data gradient runs in this library (and ReLU + 2 x 2 pooling, in one pass). Convolutions,
+Only the data gradient runs in this library (and ReLU + 2 x 2 pooling, in one pass; and the operators of the language-model
+layers at the end of this file). Convolutions,
 matrix products and the weight gradient are the framework's own operators, which is the
 integration the paper describes (Section 1: a drop-in change of the backward pass). Tensors are bf16 or fp16
 CUDA tensors; convolutions use the channels-last memory format (its physical layout is the NHWC /
 [Cout,R,S,Cin] layout of the C ABI, so nothing is copied or transposed).
 
-A layer comes in two forms with the same results. Plain calls (ordinary 16-bit CUDA tensors, integer arguments, nothing that
+Each of the first three layers comes in two forms with the same results. Plain calls (ordinary 16-bit CUDA tensors, integer arguments, nothing that
 traces or transforms the call) run as C++ autograd functions (csrc/torch_autograd.cpp): a small layer's step is bound by
 the host. Everything else runs as the Python autograd functions below: tensor subclasses and fake tensors, tracing and
 compilation, function transforms, forward-mode differentiation, strides and paddings that are not one integer, other

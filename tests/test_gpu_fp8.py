@@ -136,7 +136,7 @@ def check(y, xq, sx, wq, sw, dtype):
 @pytest.mark.parametrize("rows,features,K", [
     (1, 1, 16), (1, 128, 128), (3, 130, 144), (16, 64, 1024), (17, 256, 2048), (33, 100, 4096), (64, 520, 512), (65, 128, 384), (128, 1000, 272),
     (129, 1001, 1040), (1, 4096, 4096), (40, 2112, 2688), (300, 2048, 640), (777, 1088, 832), (1024, 8192, 512), (2048, 4096, 384),
-    (5000, 2064, 144), (4097, 4000, 128)])
+    (5000, 2064, 144), (4097, 4000, 128), (20, 20000, 4096), (9, 1100, 6000), (33, 64, 16), (300, 24, 5120), (50, 3333, 3344)])
 def test_product(dtype, rows, features, K):
     ops = operands(rows, features, K, rows + features + K)
     y = torch.full((rows, features), 7.0, dtype=TYPES[dtype], device="cuda")

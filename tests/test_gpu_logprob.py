@@ -74,7 +74,8 @@ def check(got, want, V, depth=60.0):
 @pytest.mark.parametrize("dtype", [B.BF16, B.FP16, B.FP32])
 @pytest.mark.parametrize("rows,K,classes,top", [
     (1, 1, 1, 1), (3, 2, 2, 2), (5, 7, 7, 7), (2, 8, 5, 3), (4, 64, 50, 20), (3, 255, 255, 32), (7, 257, 257, 5), (1, 2049, 2049, 32),
-    (9, 4099, 4090, 20), (600, 1000, 1000, 4), (2, 50048, 50001, 20), (1, 131072, 131072, 32), (5, 32003, 32003, 1), (300, 2112, 2100, 0)])
+    (9, 4099, 4090, 20), (600, 1000, 1000, 4), (2, 50048, 50001, 20), (1, 131072, 131072, 32), (5, 32003, 32003, 1), (300, 2112, 2100, 0), (400, 5000, 4999, 20),
+    (1300, 4100, 4100, 7), (1300, 2501, 2501, 0), (200, 9001, 9001, 32), (2, 300000, 299999, 20)])
 def test_statistics_and_alternatives(dtype, rows, K, classes, top):
     z, t = logits_of(rows, K, dtype, 17 * rows + K)
     t = t % classes
@@ -123,15 +124,16 @@ def test_fewer_numbers_than_alternatives():
     assert torch.isnan(got["top_logprob"][0]).all()
 
 
-@pytest.mark.parametrize("rows,K,k", [(2, 4096, 32), (1, 70000, 20), (400, 3000, 8)])
-def test_equal_values_go_to_the_lower_token(rows, K, k):
+@pytest.mark.parametrize("dtype", [B.BF16, B.FP32])
+@pytest.mark.parametrize("rows,K,k", [(2, 4096, 32), (1, 70000, 20), (400, 3000, 8), (1300, 5000, 20), (3, 1500, 32), (20, 200000, 32)])
+def test_equal_values_go_to_the_lower_token(dtype, rows, K, k):
     """Few distinct values: almost every comparison is a tie; and a row in ascending order, where everything enters the list."""
     g = torch.Generator().manual_seed(K)
     z = torch.randint(-3, 3, (rows, K), generator=g).float()
     z[0] = torch.arange(K) / 7.0
-    z = z.cuda()
+    z = z.to(TYPES[dtype]).cuda()
     t = torch.zeros(rows, dtype=torch.int64, device="cuda")
-    got, want = forward(z, t, None, k, B.FP32), definition(z, t, None, k)
+    got, want = forward(z, t, None, k, dtype), definition(z, t, None, k)
     assert torch.equal(got["top_token"], want["top_token"])
 
 
@@ -235,7 +237,7 @@ def test_gradient_of_rows_without_numbers():
 @pytest.mark.parametrize("n,m", [(1, 4), (2, 4), (1, 8), (2, 8), (1, 16), (2, 16), (1, 32), (2, 32)])
 @pytest.mark.parametrize("scheme", [B.RANDOM, B.MAGNITUDE, B.RESCALED_MAGNITUDE])
 def test_pruned_copy_is_algorithm_1_on_the_gradient(dtype, n, m, scheme):
-    for rows, K, classes in ((3, 160, 150), (37, 2112, 2112)):
+    for rows, K, classes in ((3, 160, 150), (37, 2112, 2112), (3, 8224, 8200), (2, 20000, 20000)):
         z, t = logits_of(rows, K, dtype, n * m)
         f = forward(z, t % classes, classes, 0, dtype)
         g = torch.randn(rows, device="cuda")
@@ -269,6 +271,24 @@ def test_streams_and_graphs():
     ref = torch.zeros_like(z)
     sdgp.sdgp_token_logprob_backward(z, t, out[2], g, grad=ref, entropy=out[1], d_entropy=g)
     assert torch.equal(ref, grad)
+
+
+def test_two_streams_at_once():
+    both = [logits_of(300, 20000, B.BF16, k) for k in (21, 22)]
+    want = [forward(z, t, None, 10) for z, t in both]
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                out = [torch.empty(300, device="cuda") for _ in range(3)]
+                tok = torch.empty(300, 10, dtype=torch.int64, device="cuda")
+                sdgp.sdgp_token_logprob(*both[k], out[0], entropy=out[1], lse=out[2], top_token=tok)
+                got[k].append((out, tok))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for out, tok in got[k]:
+            assert torch.equal(out[0].cpu(), want[k]["logprob"]) and torch.equal(out[1].cpu(), want[k]["entropy"]) and torch.equal(tok.cpu(), want[k]["top_token"])
 
 
 def test_calls_that_are_refused():

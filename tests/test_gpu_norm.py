@@ -121,7 +121,10 @@ def near(x, want, size, dtype, n):
 SHAPES = [(1, 1, 1), (2, 3, 1), (5, 8, 5), (7, 17, 1), (3, 64, 1), (33, 250, 1), (130, 256, 2), (64, 263, 8), (40, 1024, 40), (700, 520, 7),
           (19, 1999, 1), (24, 1999, 8), (1064, 1001, 8), (300, 2044, 300), (9, 4096, 1), (500, 4096, 2), (3, 8185, 3), (4, 8192, 1), (6, 8193, 2),
           (5, 16384, 1), (300, 12002, 3), (21, 1003, 7), (600, 99, 200), (2000, 36, 500), (3000, 40, 3000), (4001, 51, 4001),
-          (300, 16383, 1), (7, 20000, 1), (200, 24000, 2), (40, 32761, 1), (9, 40000, 3)]
+          (300, 16383, 1), (7, 20000, 1), (200, 24000, 2), (40, 32761, 1), (9, 40000, 3),
+          # more gates than groups of threads, for every number of threads that a row may have
+          (5000, 500, 5000), (3000, 1000, 3000), (1500, 2000, 1500), (700, 4000, 700), (400, 8000, 400), (300, 9001, 300), (1500, 1999, 1500),
+          (900, 7999, 300), (6000, 333, 3000), (1200, 4001, 400)]
 
 
 @pytest.mark.parametrize("dtype", [B.BF16, B.FP16, B.FP32])
@@ -243,6 +246,34 @@ def test_streams_and_graphs():
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(o2, out) and torch.equal(y2, y) and all(torch.equal(got[k], want[k]) for k in want)
+
+
+def test_the_sum_in_the_branchs_place():
+    for C in (256, 1001, 20000):
+        s = state(40, C, 1, B.BF16, 11)
+        out, y, post_rstd, pre_rstd = forward(s, B.BF16)
+        b = s["branch"].clone()
+        got = forward({**s, "branch": b}, B.BF16, out=b)
+        assert torch.equal(b, out) and torch.equal(got[1], y)
+
+
+def test_two_streams_at_once():
+    s = [state(500, 1999, 4, B.BF16, k) for k in (12, 13)]
+    want = []
+    for k in range(2):
+        f = forward(s[k], B.BF16)
+        want.append((f, backward(s[k], B.BF16, f[0], f[2], f[3])))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], [[], []]
+    for _ in range(5):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                f = forward(s[k], B.BF16)
+                got[k].append((f, backward(s[k], B.BF16, f[0], f[2], f[3])))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for f, g in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(f, want[k][0])) and all(torch.equal(g[n], want[k][1][n]) for n in g)
 
 
 def test_no_rows():

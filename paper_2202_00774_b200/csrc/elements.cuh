@@ -2,6 +2,7 @@
 // registers, eight at a time.
 #pragma once
 #include "prune_core.cuh"
+#include "ptx.cuh"
 
 namespace sdgp {
 namespace {
@@ -52,6 +53,23 @@ struct Element {  // DT: sdgp_dtype
       }
     }
   }
+  // The largest of eight; NaN is passed over (-infinity or NaN if there is nothing else).
+  static __device__ __forceinline__ float largest(const Raw& r, const float (&x)[8]) {
+    if constexpr (k32) {
+      return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    } else {  // two at a time
+      uint32_t m;
+      if constexpr (kF16) {
+        const __half2 h = __hmax2(__hmax2(*(const __half2*)&r.a.x, *(const __half2*)&r.a.y), __hmax2(*(const __half2*)&r.a.z, *(const __half2*)&r.a.w));
+        m = *(const uint32_t*)&h;
+      } else {
+        const __nv_bfloat162 h = __hmax2(__hmax2(*(const __nv_bfloat162*)&r.a.x, *(const __nv_bfloat162*)&r.a.y),
+                                         __hmax2(*(const __nv_bfloat162*)&r.a.z, *(const __nv_bfloat162*)&r.a.w));
+        m = *(const uint32_t*)&h;
+      }
+      return fmaxf(lane_lo<kF16>(m), lane_hi<kF16>(m));
+    }
+  }
   // Rounded to nearest even.
   static __device__ __forceinline__ Raw narrow(const float (&x)[8]) {
     Raw r;
@@ -67,6 +85,11 @@ struct Element {  // DT: sdgp_dtype
   }
   static __device__ __forceinline__ void store8(void* p, int64_t i, const Raw& r) {
     uint4* q = (uint4*)((uint8_t*)p + i * kBytes);
+    if (k32 && ((uintptr_t)q & 31u) == 0) {  // a whole sector at once
+      const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+      ptx::st_global_256(q, w);
+      return;
+    }
     q[0] = r.a;
     if (k32) q[1] = r.b;
   }

@@ -132,9 +132,7 @@ __device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row,
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       E::widen(raw[u], x[u]);
-      top_of[u] = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) top_of[u] = fmaxf(top_of[u], fmaxf(x[u][e], x[u][e + 1]));
+      top_of[u] = E::largest(raw[u], x[u]);
       most = fmaxf(most, top_of[u]);
     }
     {
@@ -178,7 +176,7 @@ __device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row,
         if (most >= least) {
 #pragma unroll
           for (int u = 0; u < kUnroll; ++u) {
-            if (top_of[u] < least) continue;
+            if (!(top_of[u] >= least)) continue;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               if (x[u][e] >= least && v0 + u * stride < nvec) {

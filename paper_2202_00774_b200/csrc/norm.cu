@@ -41,7 +41,8 @@ struct Ring {  // VECTORS: of a thread and row, in all tensors; LEAST: stages th
   static constexpr int kChunk = kCtaThreads<TPR> * 16;               // 16 bytes of each thread side by side
   static constexpr int kVec = kChunk * (Element<DT>::kBytes / 2);    // a vector: one chunk, or two of fp32
   static constexpr int kStage = VECTORS * kVec;
-  static constexpr int kRoom = (TPR > 256 ? 200 : 100) * 1024;       // (CTAs of 256 threads share a multiprocessor)
+  // of a multiprocessor's 227 KB: forward (LEAST 1) up to 1024 threads share it, backward 512
+  static constexpr int kRoom = (TPR > 512 ? 200 : LEAST == 1 ? (TPR > 256 ? 110 : 55) : TPR > 256 ? 200 : 110) * 1024;
   static constexpr int kFit = kRoom / kStage;
   static constexpr int kStages = kFit > 4 ? 4 : kFit < LEAST ? LEAST : kFit;
   static constexpr int kBytes = kStage * kStages;
@@ -63,9 +64,23 @@ __device__ __forceinline__ Part part_of(int64_t row, int C, int t) {
   return p;
 }
 
+// A thread's vector of a row to its place in a stage. fp32 vectors are two chunks: where rows are whole vectors, a warp copies its 32 vectors
+// together, 512 contiguous bytes an instruction (each its own 16 of every 32 bytes took twice the requests), so a warp has to meet
+// (__syncwarp) between the copies' arrival and their use, and between the use and the next copies.
 template <int DT, int CHUNK>
-__device__ __forceinline__ void copy_part(uint32_t dst, const void* src, int64_t row_at, const Part& p) {
+__device__ __forceinline__ void copy_part(uint32_t dst, const void* src, int64_t row_at, const Part& p, int C) {
   using E = Element<DT>;
+  if constexpr (E::k32) {
+    if (C % 8 == 0) {
+      const int lane = threadIdx.x & 31, half = lane & 1;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int other = 16 * k + (lane >> 1), at = p.first + (other - lane) * 8 + half * 4;  // that lane's vector
+        cp_async16(dst + (other - lane) * 16 + half * CHUNK, (const float*)src + row_at + (at < C ? at : 0), at < C ? 16u : 0u);
+      }
+      return;
+    }
+  }
   const uint8_t* q = (const uint8_t*)src + (row_at + p.first) * E::kBytes;
   const int bytes = p.hi * E::kBytes;
   cp_async16(dst, q, (uint32_t)min(16, bytes));
@@ -182,8 +197,8 @@ norm_kernel(const NormParams p) {
     if (row < p.rows) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + 2 * j * R::kVec, p.branch, row * p.C, part[j]);
-        copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + (2 * j + 1) * R::kVec, p.residual, row * p.C, part[j]);
+        copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + 2 * j * R::kVec, p.branch, row * p.C, part[j], p.C);
+        copy_part<DT, R::kChunk>(mine_u32 + stage * R::kStage + (2 * j + 1) * R::kVec, p.residual, row * p.C, part[j], p.C);
       }
     }
     cp_async_commit();
@@ -206,6 +221,7 @@ norm_kernel(const NormParams p) {
       for (int j = 0; j < NV; ++j) gate[j] = column_part<DT>(p.gate, at, part[j]);
     }
     cp_async_wait<R::kStages - 1>();
+    if (E::k32) __syncwarp();
     float o[NV][8], rstd = 1.0f;  // the branch, then its sum with the residual
     float s[1] = {0.0f};
 #pragma unroll
@@ -247,6 +263,7 @@ norm_kernel(const NormParams p) {
         write_part<DT>(p.y, row * p.C, part[j], E::narrow(o[j]), o[j]);
       }
     }
+    if (E::k32) __syncwarp();
     fetch(row + R::kStages * stride, stage);
     if (++stage == R::kStages) stage = 0;
   }
@@ -392,11 +409,11 @@ norm_grad_kernel(const NormGradParams p) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const uint32_t at = mine_u32 + stage * R::kStage + j * 4 * R::kVec;
-        copy_part<DT, R::kChunk>(at, p.branch, w.at, part[j]);
-        if (p.d_out) copy_part<DT, R::kChunk>(at + R::kVec, p.d_out, w.at, part[j]);
+        copy_part<DT, R::kChunk>(at, p.branch, w.at, part[j], p.C);
+        if (p.d_out) copy_part<DT, R::kChunk>(at + R::kVec, p.d_out, w.at, part[j], p.C);
         if (p.d_y) {
-          copy_part<DT, R::kChunk>(at + 2 * R::kVec, p.out, w.at, part[j]);
-          copy_part<DT, R::kChunk>(at + 3 * R::kVec, p.d_y, w.at, part[j]);
+          copy_part<DT, R::kChunk>(at + 2 * R::kVec, p.out, w.at, part[j], p.C);
+          copy_part<DT, R::kChunk>(at + 3 * R::kVec, p.d_y, w.at, part[j], p.C);
         }
       }
     }
@@ -505,6 +522,7 @@ norm_grad_kernel(const NormGradParams p) {
     }
   }
   cp_async_wait<S - 1>();
+  if (E::k32) __syncwarp();
   float own = sum_row(beside, 0, 0), own_next = own;
   meet();
 
@@ -515,6 +533,7 @@ norm_grad_kernel(const NormGradParams p) {
     load_beside(after, next.group, beside_after);
     if (next.left > 0) {
       cp_async_wait<S - 2>();
+      if (E::k32) __syncwarp();
       own_next = sum_row(beside_next, stage_next, turn ^ 1);
     }
     float s0, s1, s2;
@@ -602,6 +621,7 @@ norm_grad_kernel(const NormGradParams p) {
         }
       }
     }
+    if (E::k32) __syncwarp();
     fetch(ahead, stage);
     advance<GATES>(ahead, p, ids, step);
     here = next;

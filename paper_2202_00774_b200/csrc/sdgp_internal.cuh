@@ -132,6 +132,7 @@ cudaError_t launch_residual_norm_backward(const void* branch, const void* out, c
                                           int64_t rows, int64_t C, int64_t groups, float alpha, int n, int m, int scheme, uint64_t seed,
                                           int dtype, void* d_residual, void* d_branch, float* d_gate, float* d_post_weight,
                                           float* d_pre_weight, void* values, void* meta, float* workspace, cudaStream_t stream);
+cudaError_t take_error_norm(unsigned int* word);
 
 // Quantisation to e4m3 (fp8_quantize.cu; block_rows 1 or 128) and the product of two quantised matrices (fp8_linear.cu); K a multiple of 16.
 cudaError_t launch_fp8_quantize(const void* x, int64_t rows, int64_t K, int block_rows, int dtype, void* q, float* scale, cudaStream_t stream);

@@ -86,29 +86,44 @@ __device__ __forceinline__ void copy_part(uint32_t dst, const void* src, int64_t
   cp_async16(dst, q, (uint32_t)min(16, bytes));
   if (E::k32) cp_async16(dst + CHUNK, bytes > 16 ? q + 16 : q, (uint32_t)max(0, bytes - 16));
 }
-template <int DT, int CHUNK, bool ALIGNED>
-__device__ __forceinline__ void read_part(const uint8_t* at, const Part& p, float (&x)[8]) {
+template <int DT, int CHUNK>
+__device__ __forceinline__ void read_part(const uint8_t* at, float (&x)[8]) {
   using E = Element<DT>;
   typename E::Raw r;
   r.a = *(const uint4*)at;
   r.b = E::k32 ? *(const uint4*)(at + CHUNK) : make_uint4(0u, 0u, 0u, 0u);
   E::widen(r, x);
-  if (!ALIGNED && p.lo != 0) {  // the end of the row before (what lies behind the row was never copied and is zero)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < p.lo) x[e] = 0.0f;
+}
+// The end of the row before, copied along with a row's first vector, becomes zeros, in COUNT tensors (what lies behind the row was never
+// copied and is zero). Once a row and not where the vectors are read, which is twice, a branch each.
+template <int DT, int CHUNK, int COUNT>
+__device__ __forceinline__ void clear_before(uint8_t* at, int vector_bytes, const Part& p) {
+  using E = Element<DT>;
+  if (p.lo == 0) return;
+#pragma unroll 1
+  for (int v = 0; v < COUNT; ++v) {
+    for (int e = 0; e < p.lo; ++e) {
+      uint8_t* to = at + v * vector_bytes;
+      if (E::k32) *(float*)(to + (e >= 4 ? CHUNK : 0) + (e & 3) * 4) = 0.0f;
+      else *(uint16_t*)(to + e * 2) = 0;
+    }
   }
 }
 template <int DT, bool ALIGNED = false>
-__device__ __forceinline__ void write_part(void* dst, int64_t row_at, const Part& p, const typename Element<DT>::Raw& r, const float (&x)[8]) {
+__device__ __forceinline__ void write_part(void* dst, int64_t row_at, const Part& p, const typename Element<DT>::Raw& r) {
   using E = Element<DT>;
   const int64_t at = row_at + p.first;
   if (p.full) {
     E::store8(dst, at, r);
   } else if (!ALIGNED) {
+    const uint32_t w[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e >= p.lo && e < p.hi) E::store(dst, at + e, x[e]);
+    for (int e = 0; e < 8; ++e) {
+      if (e >= p.lo && e < p.hi) {
+        if (E::k32) ((uint32_t*)dst)[at + e] = w[e];
+        else ((uint16_t*)dst)[at + e] = (uint16_t)(w[e / 2] >> (e % 2 * 16));
+      }
+    }
   }
 }
 // The thread's elements of a vector of C elements, as they are in memory; ones where there is no vector.
@@ -222,11 +237,12 @@ norm_kernel(const NormParams p) {
     }
     cp_async_wait<R::kStages - 1>();
     if (E::k32) __syncwarp();
+    clear_before<DT, R::kChunk, 2>(mine + stage * R::kStage, R::kVec, part[0]);
     float o[NV][8], rstd = 1.0f;  // the branch, then its sum with the residual
     float s[1] = {0.0f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      read_part<DT, R::kChunk, false>(mine + stage * R::kStage + 2 * j * R::kVec, part[j], o[j]);
+      read_part<DT, R::kChunk>(mine + stage * R::kStage + 2 * j * R::kVec, o[j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[0] = fmaf(o[j][e], o[j][e], s[0]);
     }
@@ -239,7 +255,7 @@ norm_kernel(const NormParams p) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float r[8], w[8], g[8];
-      read_part<DT, R::kChunk, false>(mine + stage * R::kStage + (2 * j + 1) * R::kVec, part[j], r);
+      read_part<DT, R::kChunk>(mine + stage * R::kStage + (2 * j + 1) * R::kVec, r);
       E::widen(w_post[j], w);
       E::widen(gate[j], g);
 #pragma unroll
@@ -248,7 +264,7 @@ norm_kernel(const NormParams p) {
         o[j][e] = fmaf(g[e], n, p.alpha * r[e]);
         s[0] = fmaf(o[j][e], o[j][e], s[0]);
       }
-      write_part<DT>(p.out, row * p.C, part[j], E::narrow(o[j]), o[j]);
+      write_part<DT>(p.out, row * p.C, part[j], E::narrow(o[j]));
     }
     if (p.pre_weight) {  // (of the sums before their rounding to 16 bits)
       row_sums<TPR>(s, buffer, slot, turn);
@@ -260,7 +276,7 @@ norm_kernel(const NormParams p) {
         E::widen(w_pre[j], w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[j][e] = o[j][e] * rstd * w[e];
-        write_part<DT>(p.y, row * p.C, part[j], E::narrow(o[j]), o[j]);
+        write_part<DT>(p.y, row * p.C, part[j], E::narrow(o[j]));
       }
     }
     if (E::k32) __syncwarp();
@@ -469,16 +485,17 @@ norm_grad_kernel(const NormGradParams p) {
   const float inv_c = 1.0f / (float)p.C;
   auto sum_row = [&](const Beside& beside, int stage, int turn) -> float {
     float2 s0 = both(0.0f), s1 = both(0.0f), s2 = both(0.0f);
+    if (!ALIGNED) clear_before<DT, R::kChunk, 4>(mine + stage * R::kStage, R::kVec, part[0]);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const uint8_t* at = mine + stage * R::kStage + j * 4 * R::kVec;
       float b[8], q[8], d[8];
-      read_part<DT, R::kChunk, ALIGNED>(at, part[j], b);
+      read_part<DT, R::kChunk>(at, b);
       factors(beside, j, q);
       float o[8], y[8];
-      read_part<DT, R::kChunk, ALIGNED>(at + R::kVec, part[j], d);
-      read_part<DT, R::kChunk, ALIGNED>(at + 2 * R::kVec, part[j], o);
-      read_part<DT, R::kChunk, ALIGNED>(at + 3 * R::kVec, part[j], y);
+      read_part<DT, R::kChunk>(at + R::kVec, d);
+      read_part<DT, R::kChunk>(at + 2 * R::kVec, o);
+      read_part<DT, R::kChunk>(at + 3 * R::kVec, y);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 wd = mul2(pair_of(y, i), pair_of(w_kept[j], i)), qb = mul2(pair_of(q, i), pair_of(b, i));
@@ -583,11 +600,11 @@ norm_grad_kernel(const NormGradParams p) {
     for (int j = 0; j < NV; ++j) {
       const uint8_t* at = mine + stage * R::kStage + j * 4 * R::kVec;
       float b[8], q[8], d[8], out[8];
-      read_part<DT, R::kChunk, ALIGNED>(at, part[j], b);
+      read_part<DT, R::kChunk>(at, b);
       float o[8], y[8];
-      read_part<DT, R::kChunk, ALIGNED>(at + R::kVec, part[j], d);
-      read_part<DT, R::kChunk, ALIGNED>(at + 2 * R::kVec, part[j], o);
-      read_part<DT, R::kChunk, ALIGNED>(at + 3 * R::kVec, part[j], y);
+      read_part<DT, R::kChunk>(at + R::kVec, d);
+      read_part<DT, R::kChunk>(at + 2 * R::kVec, o);
+      read_part<DT, R::kChunk>(at + 3 * R::kVec, y);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float2 dy = pair_of(y, i), u = mul2(pair_of(o, i), both(beside.rstd));
@@ -603,7 +620,7 @@ norm_grad_kernel(const NormGradParams p) {
           out[2 * i] = x.x;
           out[2 * i + 1] = x.y;
         }
-        write_part<DT, ALIGNED>(p.d_residual, here.at, part[j], E::narrow(out), out);
+        write_part<DT, ALIGNED>(p.d_residual, here.at, part[j], E::narrow(out));
       }
       factors(beside, j, q);
 #pragma unroll
@@ -616,7 +633,7 @@ norm_grad_kernel(const NormGradParams p) {
         out[2 * i + 1] = y.y;
       }
       const typename E::Raw packed = E::narrow(out);
-      if (p.d_branch) write_part<DT, ALIGNED>(p.d_branch, here.at, part[j], packed, out);
+      if (p.d_branch) write_part<DT, ALIGNED>(p.d_branch, here.at, part[j], packed);
       if constexpr (PRUNE) {  // (rows of whole groups of 16: every part is full or empty, and a group's lanes alike)
         const int64_t vec = (here.at >> 3) + v0 + j * TPR;
         const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, t & 3);
@@ -835,12 +852,12 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_wide_kernel(const NormPa
       const Part part = part_of(row, p.C, j);
       float o[8], w[8];
       sums_of(part, o);
-      write_part<DT>(p.out, row * p.C, part, E::narrow(o), o);
+      write_part<DT>(p.out, row * p.C, part, E::narrow(o));
       if (p.pre_weight) {
         load_columns<DT>(p.pre_weight, 0, part, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = o[e] * rstd * w[e];
-        write_part<DT>(p.y, row * p.C, part, E::narrow(o), o);
+        write_part<DT>(p.y, row * p.C, part, E::narrow(o));
       }
     }
   }
@@ -917,7 +934,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
           d[e] = fmaf(-k, u[e], d[e]);
           x[e] = p.alpha * d[e];
         }
-        if (p.d_residual) write_part<DT>(p.d_residual, row * p.C, part, E::narrow(x), x);
+        if (p.d_residual) write_part<DT>(p.d_residual, row * p.C, part, E::narrow(x));
         if (p.post_sums) {
           load_columns<DT>(p.gate, (int64_t)group * p.C, part, w);
 #pragma unroll
@@ -934,7 +951,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) norm_grad_wide_kernel(const N
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = p.post_weight ? rstd_b * fmaf(q[e], d[e], -v[e] * mean) : q[e] * d[e];
         const typename E::Raw packed = E::narrow(x);
-        if (p.d_branch) write_part<DT>(p.d_branch, row * p.C, part, packed, x);
+        if (p.d_branch) write_part<DT>(p.d_branch, row * p.C, part, packed);
         if constexpr (PRUNE) {
           const int64_t vec = row * (p.C / 8) + j;
           const uint4 c = prune_any<E::kF16>(packed.a, vec, p.seed_lo, p.seed_hi, p.n, p.m, p.scheme, j & 3);

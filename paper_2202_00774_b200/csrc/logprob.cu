@@ -41,8 +41,8 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
 //
 // Keys order by value and, among equal values, by the lower index first; 0 is the key of no element. A CTA collects keys that reach a
 // bound below which k others are known to lie: to begin with, a value that k threads' largest elements reach; later, the k-th largest key
-// collected. With random logits 20 of 131072 leave some hundred keys to be sorted. (Lists kept sorted in each warp's registers, an insertion
-// at a time, took 26 us for one row of 131072 bf16 logits on a cluster of eight CTAs; 2.5 us of them without the alternatives.)
+// collected. With random logits 20 of 131072 leave some dozens of keys to be sorted. (Lists kept sorted in each warp's registers, an insertion
+// at a time, took 26 us for one row of 131072 bf16 logits on a cluster of eight CTAs; it takes 8.8 us so, 2.5 without the alternatives.)
 using Key = unsigned long long;
 
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -56,12 +56,26 @@ __device__ __forceinline__ float key_value(Key k) {
 }
 
 constexpr int kMostKeys = 512;      // that a CTA collects
-constexpr int kSortAbove = 48;      // as many are sorted out: a higher bound lets fewer of what follows in (4096 x 131072, top 20: 329 us, 383 with 128)
+constexpr int kSortAbove = 48;      // as many are sorted out: a higher bound lets fewer of what follows in
 
 struct Candidates {
   Key keys[kMostKeys];
   Key best[32];
-  uint32_t bound[16];
+  uint32_t bound[96], least;  // of find_bound, at most 64 + 15 and four
+  int count;
+};
+
+// Where a row takes a CTA several rounds, a meeting in each of them and the keys of lower bounds cost as much as the sums do (top 20 of
+// 4096 x 131072 bf16: 324 us, and 180 without). There only the largest element of each thread's part of some rounds is kept; the threads'
+// largest give the bound once the row has been read, and the few parts that reach it are read again: 208 us; 256 rows 31.7 -> 19.7 us. A
+// row of one round has its elements still in registers (on a cluster 10.3 us, 11.9 so), and a warp's own rows need no meeting.
+enum Top { kNone, kAlong, kBehind };  // alternatives: none, found as the row is read or behind it
+constexpr int kMostHits = 128;
+template <int NT>
+struct Parts {
+  static constexpr int kEach = NT > 256 ? 16 : 32;  // parts of a thread
+  float most[kEach * NT];
+  uint32_t hits[kMostHits];
   int count;
 };
 
@@ -100,8 +114,8 @@ constexpr int kMostParts = 8;
 
 // A cluster of CTAs (one where there are rows enough for all multiprocessors) reads a row in slices; its first CTA joins what the others found
 // through distributed shared memory.
-template <int DT, bool TOP, int NT>
-__device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row, Stats* stats, Candidates& c) {
+template <int DT, int TOP, int NT>  // TOP: a Top
+__device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row, Stats* stats, Candidates& c, Parts<NT>* seen) {
   using E = Element<DT>;
   constexpr int kWarps = NT / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -117,24 +131,124 @@ __device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row,
   float2 s = {0.0f, 0.0f}, t = {0.0f, 0.0f};  // sums of even and of odd elements
   Key bound = 0;
   int held = 0;  // keys of the rounds before
-  if (TOP && threadIdx.x == 0) c.count = 0;
+  if (TOP && threadIdx.x == 0) {
+    c.count = 0;
+    if (TOP == kBehind) seen->count = 0;
+  }
 
   // the CTA's slice, a round of it at a time (the same number of rounds in all its warps: the candidates meet at barriers)
   const int stride = (int)parts * NT, first = (int)part * NT;
   const int rounds = nvec > first ? (nvec - first + stride * kUnroll - 1) / (stride * kUnroll) : 0;
-  for (int round = 0; round < rounds; ++round) {
-    const int v0 = first + round * stride * kUnroll + (int)threadIdx.x;
-    typename E::Raw raw[kUnroll];
+  typename E::Raw raw[kUnroll];
+  float x[kUnroll][8], top_of[kUnroll], most;
+  auto load_round = [&](int v0) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) raw[u] = v0 + u * stride < nvec ? E::load8(body, (int64_t)(v0 + u * stride) * 8) : E::lowest8();
-    float x[kUnroll][8], top_of[kUnroll];
-    float most = -INFINITY;
+    most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       E::widen(raw[u], x[u]);
       top_of[u] = E::largest(raw[u], x[u]);
       most = fmaxf(most, top_of[u]);
     }
+  };
+  // A value that at least `top` elements reach. Few warps: ceil(top / warps) lanes of each reach the least of their bounds. Many: the least of
+  // all would let several times as many keys in, so it is the top-th of the largest elements of about 2 top lanes, for two rounds of compares
+  // and a barrier (131072 bf16 on a cluster of CTAs of 16 warps: 10.3 -> 9.1 us; 16384 x 4000 fp32, CTAs of four: 100 us, 107 with the latter).
+  auto find_bound = [&](float largest) {
+    constexpr bool kRanked = kWarps >= 8;
+    const int with = min(kWarps, (nvec - first + 31) / 32), each = kRanked ? min(32, (2 * p.top + with - 1) / with) : (p.top + with - 1) / with;
+    uint32_t mine = first + (int)threadIdx.x < nvec ? ordered(largest) : 0u, reached = 0u;
+    for (int i = 0; i < each; ++i) {
+      reached = __reduce_max_sync(0xFFFFFFFFu, mine);
+      if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, mine == reached)) - 1) mine = 0u;
+      if (kRanked && lane == 0 && warp < with) c.bound[warp * each + i] = reached;
+    }
+    if constexpr (kRanked) {
+      const int n = with * each;
+      if (threadIdx.x < 4) c.bound[n + threadIdx.x] = 0u;
+      __syncthreads();
+      if ((int)threadIdx.x < n) {
+        const uint32_t v = c.bound[threadIdx.x];
+        int above = 0, reach = 0;
+        for (int j = 0; j < n; j += 4) {
+          const uint4 o = *(const uint4*)&c.bound[j];
+          above += (o.x > v) + (o.y > v) + (o.z > v) + (o.w > v);
+          reach += (o.x >= v) + (o.y >= v) + (o.z >= v) + (o.w >= v);
+        }
+        if (above < p.top && p.top <= reach) c.least = v;  // (equal ones write the same)
+      }
+      __syncthreads();
+      reached = c.least;
+    } else {
+      if (lane == 0) c.bound[warp] = reached;
+      __syncthreads();
+      reached = 0xFFFFFFFFu;
+      for (int w = 0; w < with; ++w) reached = min(reached, c.bound[w]);
+    }
+    bound = (Key)reached << 32;
+  };
+  auto add_keys = [&](const float (&v)[8], int vec) {  // of a vector of eight
+    const float least = bound ? key_value(bound) : -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (v[e] >= least) {
+        const Key k = make_key(v[e], (uint32_t)(head + vec * 8 + e));
+        if (k >= bound) {
+          const int at = atomicAdd(&c.count, 1);
+          if (at < kMostKeys) c.keys[at] = k;
+        }
+      }
+    }
+  };
+  // the keys of a round, by all threads
+  auto meet = [&](int v0) {
+    for (;;) {
+      const float least = bound ? key_value(bound) : -INFINITY;
+      bool added = false;
+      if (most >= least) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+          if (!(top_of[u] >= least)) continue;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (x[u][e] >= least && v0 + u * stride < nvec) {
+              const Key k = make_key(x[u][e], (uint32_t)(head + (v0 + u * stride) * 8 + e));
+              if (k >= bound) {
+                const int at = atomicAdd(&c.count, 1);
+                if (at < kMostKeys) c.keys[at] = k;
+                added = true;
+              }
+            }
+          }
+        }
+      }
+      if (!__syncthreads_or(added)) break;
+      const int n = c.count;
+      __syncthreads();
+      if (n <= kSortAbove) {
+        held = n;
+        break;
+      }
+      sort_out<NT>(c, min(n, kMostKeys), p.top);
+      bound = c.best[p.top - 1];
+      // all of them seen: the best stay. More than there is room for: this round again, from what was there before it, with the higher bound
+      // (at least kMostKeys - 32 elements lie below that, so a round ends)
+      const bool again = n > kMostKeys;
+      if (!again && threadIdx.x < p.top) c.keys[threadIdx.x] = c.best[threadIdx.x];
+      if (!again) held = p.top;
+      if (threadIdx.x == 0) c.count = held;
+      __syncthreads();
+      if (!again) break;
+    }
+  };
+
+  float part_most = -INFINITY;
+  int part_rounds = 0, parts_seen = 0;
+  const int rounds_each = (rounds + Parts<NT>::kEach - 1) / Parts<NT>::kEach;
+  for (int round = 0; round < rounds; ++round) {
+    const int v0 = first + round * stride * kUnroll + (int)threadIdx.x;
+    load_round(v0);
     {
       const float old = m;
       m = fmaxf(m, most);
@@ -155,58 +269,54 @@ __device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row,
         }
       }
     }
-    if constexpr (TOP) {
-      if (round == 0) {
-        // ceil(top / warps) lanes of each warp that has elements reach the warp's bound, so `top` elements reach the least of them
-        const int with = min(kWarps, (nvec - first + 31) / 32), each = (p.top + with - 1) / with;
-        uint32_t mine = v0 < nvec ? ordered(most) : 0u, reached = 0u;
-        for (int i = 0; i < each; ++i) {
-          reached = __reduce_max_sync(0xFFFFFFFFu, mine);
-          if (lane == __ffs(__ballot_sync(0xFFFFFFFFu, mine == reached)) - 1) mine = 0u;
-        }
-        if (lane == 0) c.bound[warp] = reached;
-        __syncthreads();
-        reached = 0xFFFFFFFFu;
-        for (int w = 0; w < with; ++w) reached = min(reached, c.bound[w]);
-        bound = (Key)reached << 32;
+    if constexpr (TOP == kAlong) {
+      if (round == 0) find_bound(most);
+      meet(v0);
+    }
+    if constexpr (TOP == kBehind) {
+      part_most = fmaxf(part_most, most);
+      if (++part_rounds == rounds_each || round + 1 == rounds) {
+        seen->most[parts_seen++ * NT + threadIdx.x] = part_most;
+        part_most = -INFINITY;
+        part_rounds = 0;
       }
-      for (;;) {
-        const float least = bound ? key_value(bound) : -INFINITY;
-        bool added = false;
-        if (most >= least) {
-#pragma unroll
-          for (int u = 0; u < kUnroll; ++u) {
-            if (!(top_of[u] >= least)) continue;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (x[u][e] >= least && v0 + u * stride < nvec) {
-                const Key k = make_key(x[u][e], (uint32_t)(head + (v0 + u * stride) * 8 + e));
-                if (k >= bound) {
-                  const int at = atomicAdd(&c.count, 1);
-                  if (at < kMostKeys) c.keys[at] = k;
-                  added = true;
-                }
-              }
-            }
-          }
+    }
+  }
+  if constexpr (TOP == kBehind) {
+    if (rounds > 0) {
+      find_bound(m);
+      const float least = bound ? key_value(bound) : -INFINITY;
+      for (int i = 0; i < parts_seen; ++i) {
+        if (seen->most[i * NT + threadIdx.x] >= least) {
+          const int at = atomicAdd(&seen->count, 1);
+          if (at < kMostHits) seen->hits[at] = (uint32_t)(i * NT + (int)threadIdx.x);
         }
-        if (!__syncthreads_or(added)) break;
-        const int n = c.count;
-        __syncthreads();
-        if (n <= kSortAbove) {
-          held = n;
-          break;
+      }
+      __syncthreads();
+      const int hits = seen->count;
+      if (hits <= kMostHits) {
+        const int vectors = rounds_each * kUnroll;  // of a part
+        for (int i = threadIdx.x; i < hits * vectors; i += NT) {
+          const int hit = (int)seen->hits[i / vectors], of = i % vectors;
+          const int64_t vec = first + ((int64_t)(hit / NT) * vectors + of) * stride + hit % NT;
+          if (vec >= nvec) continue;
+          float v[8];
+          E::widen(E::load8(body, vec * 8), v);
+          add_keys(v, (int)vec);
         }
-        sort_out<NT>(c, min(n, kMostKeys), p.top);
-        bound = c.best[p.top - 1];
-        // all of them seen: the best stay. More than there is room for: this round again, from what was there before it, with the higher bound
-        // (at least kMostKeys - 32 elements lie below that, so a round ends)
-        const bool again = n > kMostKeys;
-        if (!again && threadIdx.x < p.top) c.keys[threadIdx.x] = c.best[threadIdx.x];
-        if (!again) held = p.top;
-        if (threadIdx.x == 0) c.count = held;
         __syncthreads();
-        if (!again) break;
+      }
+      held = c.count;
+      if (hits > kMostHits || held > kMostKeys - 32) {  // equal elements: round by round, so that the lowest indexes stay
+        __syncthreads();
+        if (threadIdx.x == 0) c.count = 0;
+        held = 0;
+        __syncthreads();
+        for (int round = 0; round < rounds; ++round) {
+          const int v0 = first + round * stride * kUnroll + (int)threadIdx.x;
+          load_round(v0);
+          meet(v0);
+        }
       }
     }
   }
@@ -283,20 +393,23 @@ __device__ __forceinline__ void logprob_row(const LogprobParams& p, int64_t row,
   }
 }
 
-template <int DT, bool TOP, int NT>
+template <int DT, int TOP, int NT>
 __global__ void __launch_bounds__(NT, NT == 32 ? 24 : 1024 / NT)
 logprob_kernel(const LogprobParams p) {
   __shared__ Stats stats[NT / 32];
   __shared__ __align__(16) Candidates found;
+  constexpr bool kParts = TOP == kBehind;
+  __shared__ __align__(16) uint8_t parts_room[kParts ? sizeof(Parts<NT>) : 16];
+  Parts<NT>* seen = kParts ? (Parts<NT>*)parts_room : nullptr;
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
   if constexpr (NT == 32) {  // (as many CTAs as fit; one for each row, 16384 short rows took 18 us to be dealt out)
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-      logprob_row<DT, TOP, NT>(p, row, stats, found);
+      logprob_row<DT, TOP, NT>(p, row, stats, found, seen);
       __syncwarp();
     }
   } else {
-    logprob_row<DT, TOP, NT>(p, blockIdx.x / ptx::cluster_nctarank(), stats, found);
+    logprob_row<DT, TOP, NT>(p, blockIdx.x / ptx::cluster_nctarank(), stats, found, seen);
   }
 }
 
@@ -577,8 +690,15 @@ constexpr int kWarpRow = 2048;  // tokens up to which a row is one warp's
 
 template <int DT, int NT>
 cudaError_t launch_logprob_rows(const LogprobParams& p, int64_t rows, int cluster, cudaStream_t stream) {
-  return p.top > 0 ? launch(logprob_kernel<DT, true, NT>, rows * cluster, NT, cluster, stream, p)
-                   : launch(logprob_kernel<DT, false, NT>, rows * cluster, NT, cluster, stream, p);
+  if (p.top == 0) return launch(logprob_kernel<DT, kNone, NT>, rows * cluster, NT, cluster, stream, p);
+  if constexpr (NT == 32) {
+    return launch(logprob_kernel<DT, kAlong, NT>, rows * cluster, NT, cluster, stream, p);
+  } else {
+    if constexpr (NT == 512) {
+      if (p.classes <= cluster * NT * kUnroll * 8) return launch(logprob_kernel<DT, kAlong, NT>, rows * cluster, NT, cluster, stream, p);
+    }
+    return launch(logprob_kernel<DT, kBehind, NT>, rows * cluster, NT, cluster, stream, p);
+  }
 }
 
 template <int DT>

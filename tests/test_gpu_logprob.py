@@ -137,6 +137,45 @@ def test_equal_values_go_to_the_lower_token(dtype, rows, K, k):
     assert torch.equal(got["top_token"], want["top_token"])
 
 
+@pytest.mark.parametrize("dtype", [B.BF16, B.FP32])
+@pytest.mark.parametrize("rows,K,pad", [(1300, 5000, 0), (1200, 140001, 7), (400, 20000, 3), (150, 300001, 0), (20, 40000, 0), (2, 2500003, 5), (14, 1999, 1)])
+def test_alternatives_wherever_the_largest_lie(dtype, rows, K, pad):
+    """Rows of every kind: random, one value, descending, ascending, almost all masked, few distinct values, numbers that are none,
+    the largest side by side in the middle; parts of a row that one thread reads are one or several rounds."""
+    g = torch.Generator(device="cuda").manual_seed(K)
+    z = torch.randn(rows, K + pad, generator=g, device="cuda") * 2.5
+    ramp = torch.arange(K + pad, device="cuda") / 64.0
+    for kind in range(1, 8):
+        some = slice(kind if rows > 8 else kind % rows, None, 8)
+        if rows <= 8 and kind not in (3, 7):
+            continue
+        if kind == 1:
+            z[some] = 1.5
+        elif kind == 2:
+            z[some] = -ramp
+        elif kind == 3:
+            z[some] = ramp
+        elif kind == 4:
+            z[some, : K // 2] = -float("inf")
+            z[some, K // 2 + 11:] = -float("inf")
+        elif kind == 5:
+            z[some] = torch.round(z[some])
+        elif kind == 6:
+            z[some, ::3] = float("nan")
+        else:
+            z[some, K // 2: K // 2 + 77] += 40.0
+    z = z.to(TYPES[dtype])
+    z[:, K:] = float("inf")                  # behind the classes: not looked at
+    t = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    numbers = torch.where(torch.isnan(z[:, :K]), -float("inf"), z[:, :K].float())
+    order = torch.cat([torch.sort(part, dim=1, descending=True, stable=True).indices[:, :32] for part in numbers.split(64)])
+    for top in (1, 20, 32):
+        tok = torch.empty(rows, top, dtype=torch.int64, device="cuda")
+        lp, out = torch.empty(rows, device="cuda"), torch.empty(rows, top, device="cuda")
+        sdgp.sdgp_token_logprob(z, t, lp, classes=K, dtype=dtype, top_token=tok, top_logprob=out)
+        assert torch.equal(tok, order[:, :top]), (tok != order[:, :top]).nonzero()[:5]
+
+
 def test_outputs_that_are_not_asked_for():
     z, t = logits_of(5, 1000, B.BF16, 1)
     lp = torch.empty(5, device="cuda")

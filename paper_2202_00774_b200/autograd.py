@@ -14,6 +14,10 @@ traces or transforms the call) run as C++ autograd functions (csrc/torch_autogra
 the host. Everything else runs as the Python autograd functions below: tensor subclasses and fake tensors, tracing and
 compilation, function transforms, forward-mode differentiation, strides and paddings that are not one integer, other
 devices and element types.
+
+A step that is captured into a CUDA graph needs leaves without an eager graph that still lives: drop the outputs of earlier eager steps first.
+torch keeps a leaf's gradient accumulator, with the stream that it was made on, for as long as any graph holds it, and waiting for that
+stream inside a capture is an error that torch does not survive.
 """
 from __future__ import annotations
 
@@ -350,4 +354,6 @@ def sdgp_linear_fp8(x, weight, quantized=None, n=2, m=4, scheme=_b.MAGNITUDE, se
     weight gradient uses the unpruned dL/dO. ``quantized``: what ``sdgp_fp8_weights(weight)`` gave. in_features and out_features
     must be multiples of 64."""
     wq, w_scale = sdgp_fp8_weights(weight) if quantized is None else quantized
+    if wq.shape != weight.shape:
+        raise ValueError(f"sdgp_linear_fp8: quantized weights of shape {tuple(wq.shape)} for weights of shape {tuple(weight.shape)}")
     return _SDGPLinearFp8Fn.apply(x, weight, wq, w_scale, n, m, scheme, seed)

@@ -115,3 +115,12 @@ def linear(lib, xq=A, x_scale=A, wq=A, w_scale=A, y=A, rows=4, features=64, K=64
     (ALIGNMENT, dict(w_scale=ODD)), (OK, dict(rows=0, xq=None)), (OK, dict(features=0, wq=None))])
 def test_fp8_linear(lib, status, change):
     assert linear(lib, **change) == status
+
+
+def test_quantized_weights_of_another_shape_are_refused():
+    import torch
+    from paper_2202_00774_b200.autograd import sdgp_linear_fp8
+    x, w = torch.zeros(2, 128, dtype=torch.bfloat16), torch.zeros(256, 128, dtype=torch.bfloat16)
+    q, scale = torch.zeros(128, 128, dtype=torch.uint8), torch.ones(1, 1)
+    with pytest.raises(ValueError, match="shape"):
+        sdgp_linear_fp8(x, w, quantized=(q, scale))

@@ -686,7 +686,7 @@ norm_grad_kernel(const NormGradParams p) {
   }
 }
 
-// Sums of those sums, in a fixed order. A CTA takes 32 columns: with its 32 lines of threads either one line of sums of the slots each
+// Sums of those sums, in a fixed order. A CTA takes 32 columns: with its lines of threads either one line of sums of the slots each
 // (job 0: d_pre_weight; job 1, with GATES: d_post_weight) or, job 2, groups and their units: d_gate = w_post sum d v of each group and, without
 // GATES, d_post_weight = sum over groups of g sum d v.
 struct SumParams {
@@ -696,9 +696,10 @@ struct SumParams {
   int64_t rows_per_group, groups;
   int C, pitch, slots, splits, gate_rows;
   bool shifted;  // lines of sums start at the place of their first row in its vector
-  int job0, jobs;
+  int jobs;
+  uint32_t order;  // of the jobs, four bits each
 };
-constexpr int kSumLines = 32;
+constexpr int kSumLines = 32;  // of threads of a CTA, at most
 
 __device__ __forceinline__ float sum_lines(float (*part)[33], float s, int from, int n) {  // over lines [from, from + n), in order
   part[threadIdx.y][threadIdx.x] = s;
@@ -723,30 +724,28 @@ __device__ __forceinline__ float sum_of_lines(int first, int stride, int n, Line
   return s;
 }
 
-template <int DT>
-__global__ void __launch_bounds__(32 * kSumLines) norm_sums_kernel(const SumParams p) {
+template <int DT, int LINES>
+__global__ void __launch_bounds__(32 * LINES) norm_sums_kernel(const SumParams p) {
   using E = Element<DT>;
-  __shared__ float part[kSumLines][33];
+  __shared__ float part[LINES][33];
   ptx::wait_for_previous_grid();
   ptx::launch_dependents();
-  const int job = p.job0 + (int)blockIdx.x % p.jobs, c = (int)(blockIdx.x / p.jobs) * 32 + threadIdx.x, line = threadIdx.y;
+  const int job = (int)(p.order >> 4 * (blockIdx.x % (uint32_t)p.jobs) & 15u), c = (int)(blockIdx.x / p.jobs) * 32 + threadIdx.x, line = threadIdx.y;
   const bool on = c < p.C;
   auto place = [&](int64_t row) { return (int)((uint64_t)row * (uint64_t)p.C & 7u); };  // of a line of sums whose first row this is
   if (job < 2) {
     const float* src = job == 0 ? p.pre_sums : p.post_sums;
-    if (!src) return;
     float s = 0.0f;
-    if (on && !p.shifted) s = sum_of_lines(line, kSumLines, p.slots, [&](int i) { return src + (int64_t)i * p.pitch + c; });
+    if (on && !p.shifted) s = sum_of_lines(line, LINES, p.slots, [&](int i) { return src + (int64_t)i * p.pitch + c; });
     else if (on)
-      s = sum_of_lines(line, kSumLines, p.slots, [&](int i) {
+      s = sum_of_lines(line, LINES, p.slots, [&](int i) {
         const int group = i / p.splits;
         return src + (int64_t)i * p.pitch + place((int64_t)group * p.rows_per_group + (i - group * p.splits)) + c;
       });
-    s = sum_lines(part, s, 0, kSumLines);
+    s = sum_lines(part, s, 0, LINES);
     if (on && line == 0) (job == 0 ? p.d_pre_weight : p.d_post_weight)[c] = s;
     return;
   }
-  if (!p.unit_sums) return;
   auto sum_of_group = [&](int64_t g, int first, int stride) {
     return sum_of_lines(first, stride, p.gate_rows, [&](int i) {
       return p.unit_sums + (g * p.gate_rows + i) * p.pitch + (p.shifted ? place(g * p.rows_per_group + i) : 0) + c;
@@ -754,8 +753,8 @@ __global__ void __launch_bounds__(32 * kSumLines) norm_sums_kernel(const SumPara
   };
   // as many groups at a time as there are lines, or several lines for each group
   int at_once = 1;
-  while (at_once < kSumLines && at_once < p.groups) at_once *= 2;
-  const int each = kSumLines / at_once, mine = line / each;
+  while (at_once < LINES && at_once < p.groups) at_once *= 2;
+  const int each = LINES / at_once, mine = line / each;
   const float w = on && p.post_weight ? E::load(p.post_weight, c) : 1.0f;
   float post = 0.0f;
   for (int64_t g = mine; g - mine < p.groups; g += at_once) {
@@ -769,7 +768,7 @@ __global__ void __launch_bounds__(32 * kSumLines) norm_sums_kernel(const SumPara
     }
   }
   if (p.d_post_weight && !p.post_sums) {
-    post = sum_lines(part, post, 0, kSumLines);
+    post = sum_lines(part, post, 0, LINES);
     if (on && line == 0) p.d_post_weight[c] = post;
   }
 }
@@ -1142,6 +1141,13 @@ cudaError_t launch_backward(const NormGradParams& p, const Plan& plan, cudaStrea
   return launch_backward_form<DT, true, false>(p, plan, stream);
 }
 
+template <int DT>
+cudaError_t launch_sums(const SumParams& p, int64_t ctas, int lines, cudaStream_t stream) {
+  if (lines == 8) return launch<norm_sums_kernel<DT, 8>>(ctas, dim3(32, 8), 0, 1, stream, p);
+  if (lines == 16) return launch<norm_sums_kernel<DT, 16>>(ctas, dim3(32, 16), 0, 1, stream, p);
+  return launch<norm_sums_kernel<DT, kSumLines>>(ctas, dim3(32, kSumLines), 0, 1, stream, p);
+}
+
 }  // namespace
 
 cudaError_t take_error_norm(unsigned int* word) { return take_error_word(word); }
@@ -1187,14 +1193,18 @@ cudaError_t launch_residual_norm_backward(const void* branch, const void* out, c
                                              : launch_backward<SDGP_FP32>(p, plan, stream);
   if (e != cudaSuccess || (!pre_sums && !post_sums && !unit_sums)) return e;
   SumParams q = {pre_sums, post_sums, unit_sums, gate, post_weight, d_pre_weight, d_post_weight, d_gate, rows / groups, groups, (int)C,
-                 (int)pitch, plan.ids(), plan.splits, plan.gate_rows, plan.tpr != 0 && plan.period != 1, 0, 0};
-  q.job0 = pre_sums ? 0 : post_sums ? 1 : 2;
-  q.jobs = (unit_sums ? 3 : post_sums ? 2 : 1) - q.job0;
-  const int64_t ctas = q.jobs * ((C + 31) / 32);
-  const dim3 block(32, kSumLines);
-  if (dtype == SDGP_BF16) return launch<norm_sums_kernel<SDGP_BF16>>(ctas, block, 0, 1, stream, q);
-  if (dtype == SDGP_FP16) return launch<norm_sums_kernel<SDGP_FP16>>(ctas, block, 0, 1, stream, q);
-  return launch<norm_sums_kernel<SDGP_FP32>>(ctas, block, 0, 1, stream, q);
+                 (int)pitch, plan.ids(), plan.splits, plan.gate_rows, plan.tpr != 0 && plan.period != 1, 0, 0u};
+  const bool present[3] = {pre_sums != nullptr, post_sums != nullptr, unit_sums != nullptr};
+  for (uint32_t job = 0; job < 3; ++job)
+    if (present[job]) q.order |= job << 4 * q.jobs++;
+  // As many lines of threads as let the CTAs of two jobs run at once (16384 columns: 31 us with 32 lines everywhere). Not by the jobs that there
+  // are: which sums are asked for changes none of them.
+  const int64_t columns = (C + 31) / 32, ctas = q.jobs * columns;
+  int lines = kSumLines;
+  while (lines > 8 && 2 * columns * 32 * lines > (int64_t)sm_count() * 2048) lines /= 2;
+  return dtype == SDGP_BF16   ? launch_sums<SDGP_BF16>(q, ctas, lines, stream)
+         : dtype == SDGP_FP16 ? launch_sums<SDGP_FP16>(q, ctas, lines, stream)
+                              : launch_sums<SDGP_FP32>(q, ctas, lines, stream);
 }
 
 }  // namespace sdgp

@@ -176,6 +176,15 @@ def test_alternatives_wherever_the_largest_lie(dtype, rows, K, pad):
         assert torch.equal(tok, order[:, :top]), (tok != order[:, :top]).nonzero()[:5]
 
 
+@pytest.mark.parametrize("rows,K", [(1, 131072), (200, 70000), (500, 30000), (2500, 9000), (3000, 1500)])
+def test_alternatives_repeat_themselves(rows, K):
+    z, t = logits_of(rows, K, B.BF16, K)
+    want = forward(z, t, None, 20, B.BF16)
+    for _ in range(20):
+        got = forward(z, t, None, 20, B.BF16)
+        assert all(torch.equal(got[k], want[k]) for k in want)
+
+
 def test_outputs_that_are_not_asked_for():
     z, t = logits_of(5, 1000, B.BF16, 1)
     lp = torch.empty(5, device="cuda")

@@ -276,6 +276,23 @@ def test_two_streams_at_once():
             assert all(torch.equal(a, b) for a, b in zip(f, want[k][0])) and all(torch.equal(g[n], want[k][1][n]) for n in g)
 
 
+@pytest.mark.parametrize("dtype", [B.BF16, B.FP32])
+@pytest.mark.parametrize("rows,C", [(300, 9000), (500, 16384), (261, 12007), (150, 32760), (1, 16384)])
+def test_rows_of_several_ctas_repeat_themselves(dtype, rows, C):
+    """Rows that a cluster shares: every call gives the same bits, also with two streams at work, and no wait runs out."""
+    s = state(rows, C, 1, dtype, C + rows)
+    f = forward(s, dtype)
+    want = backward(s, dtype, f[0], f[2], f[3])
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(20):
+        with torch.cuda.stream(streams[i % 2]):
+            got.append(backward(s, dtype, f[0], f[2], f[3]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g[n], want[n]) for g in got for n in g)
+    assert sdgp.sdgp_last_device_error() == 0
+
+
 def test_no_rows():
     s = state(0, 64, 1, B.BF16, 9)
     g = {k: torch.full(sh, 5.0, device="cuda") for k, sh in (("d_gate", (1, 64)), ("d_post_weight", (64,)), ("d_pre_weight", (64,)))}

@@ -385,10 +385,11 @@ __device__ __forceinline__ float warp_sums3(float a, float b, float c) {
 //
 // GATES: a slot's rows have more than one gate, so gates go along with the rows. Else q = g w_post stays in registers, and a thread has
 // room for NV = 2 vectors, TPR threads apart: half the exchanges, addresses and barriers an element.
-// CL: CTAs that share rows too wide for one. Each sends its warps' sums to all, into one of three places in turn, and an mbarrier of each
-// place counts them: a warp sends a row's sums after it has read those of three rows before, and reads a row's after all have sent them, so
-// no place is written too early. (With a barrier of the cluster a row, which waits for the outputs of all rows before: 313 us for
-// 4096 x 8192 fp32, 217 now.)
+// CL: CTAs that share rows too wide for one. Each sends its warps' sums to all, into one of four places in turn, and an mbarrier of each
+// place counts them. A warp sends row i + 4's sums, into the place of row i, after it has read those of row i + 2. All warps have sent those by
+// then, and each did so after it had read row i's: no place is written before everyone has read it, and no sums are counted on the phase of an
+// earlier row. (Three places are too few: the sender of row i + 3 has read row i + 1, whose sums a warp sends before it reads row i's.)
+// (With a barrier of the cluster a row, which waits for the outputs of all rows before: 313 us for 4096 x 8192 fp32, 222 now.)
 constexpr unsigned kSumsError = 0x100u;  // in the error word: sums that did not come
 template <int DT, int TPR, int NV, int CL, bool GATES, bool ALIGNED, bool PRUNE>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, TPR > 256 ? 1 : 2)
@@ -396,7 +397,7 @@ norm_grad_kernel(const NormGradParams p) {
   using E = Element<DT>;
   using R = Ring<DT, TPR, 4 * NV, 2>;
   constexpr int SLOTS = kCtaThreads<TPR> / TPR, S = R::kStages, W = TPR / 32, WC = W * CL;  // WC: warps of a row
-  constexpr int PLACES = CL > 1 ? 3 : 2;
+  constexpr int PLACES = CL > 1 ? 4 : 2;
   constexpr uint32_t kSumBytes = 3 * WC * sizeof(float);
   static_assert(CL == 1 || SLOTS == 1, "");
   extern __shared__ __align__(16) uint8_t ring[];

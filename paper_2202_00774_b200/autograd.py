@@ -179,14 +179,15 @@ def sdgp_conv2d_relu(x, weight, stride=1, padding=0, pool=False, n=2, m=4, schem
 
 def _linear_grads(ctx, dO, vals, meta, x, weight, need_x, need_w, pattern):
     """Input and weight gradient of ``x @ weight.T`` from the unpruned dL/dO [rows, K] and, where the pass that made it has
-    written one, its compressed pruned copy."""
+    written one, its compressed pruned copy. Both products are of dL/dO's type: weights or activations of another one (fp32 weights of
+    the 8-bit layer, operands that autocast has rounded) are rounded to it."""
     n, m, scheme, seed = pattern
     grad_x = grad_w = None
     if need_x:
         rows, K = dO.shape
         N = weight.shape[1]
         dt = _dtype_code(dO)
-        W = weight.contiguous()
+        W = weight.to(dO.dtype).contiguous()
         dD = torch.empty((rows, N), dtype=dO.dtype, device=dO.device)
         with torch.cuda.device(dO.device):
             if vals is not None:
@@ -195,9 +196,9 @@ def _linear_grads(ctx, dO, vals, meta, x, weight, need_x, need_w, pattern):
                 flags = _b.FLAG_TWO_PASS if n <= 2 or n == m else _b.FLAG_MASKED
                 ws = torch.empty(max(16, _b.sdgp_workspace_size_linear(rows, K, N, flags)), dtype=torch.uint8, device=dO.device)
                 _b.sdgp_dgrad_linear_typed(dO, W, dD, n, m, scheme, seed, dt, workspace=ws, flags=flags)
-        grad_x = dD.reshape(x.shape)
+        grad_x = dD.reshape(x.shape).to(x.dtype)
     if need_w:
-        grad_w = dO.t() @ x.reshape(-1, x.shape[-1])   # unpruned dL/dO (Section 3.1)
+        grad_w = (dO.t() @ x.reshape(-1, x.shape[-1]).to(dO.dtype)).to(weight.dtype)   # unpruned dL/dO (Section 3.1)
     return grad_x, grad_w
 
 
@@ -352,7 +353,8 @@ def sdgp_linear_fp8(x, weight, quantized=None, n=2, m=4, scheme=_b.MAGNITUDE, se
     """``x @ weight.T`` in 8 bits - both quantised to e4m3 with a scale for each block of 128 - whose backward pass is that of
     ``sdgp_linear``: the roundings pass the gradient through, the input gradient is ``prune(dL/dO) @ weight`` in 16 bits, the
     weight gradient uses the unpruned dL/dO. ``quantized``: what ``sdgp_fp8_weights(weight)`` gave. in_features and out_features
-    must be multiples of 64."""
+    must be multiples of 64. ``x`` is bf16 or fp16; ``weight`` may be of another type (fp32 master weights): it is quantised as it is, and
+    rounded to ``x``'s type for the input gradient."""
     wq, w_scale = sdgp_fp8_weights(weight) if quantized is None else quantized
     if wq.shape != weight.shape:
         raise ValueError(f"sdgp_linear_fp8: quantized weights of shape {tuple(wq.shape)} for weights of shape {tuple(weight.shape)}")

@@ -266,7 +266,8 @@ def sdgp_channel_scales(dO, n, m, dtype, out):
 
 
 # ---- operators around a language model's linear layers: the work goes to the current stream of the tensors' device, whichever
-# device is current; element types are checked against `dtype` ----
+# device is current; element types are checked against `dtype` (int16 and uint16 tensors are taken as the bits of 16-bit elements, uint8
+# tensors as those of e4m3 numbers) ----
 
 
 def sdgp_token_logprob(logits, targets, logprob, entropy=None, lse=None, top_logprob=None, top_token=None, classes=None, dtype=BF16):

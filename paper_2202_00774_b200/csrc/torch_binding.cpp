@@ -294,11 +294,27 @@ struct LmArgs : Args {
     any = true;
     return t;
   }
-  // Elements of `dtype`: 16-bit (any type, as elsewhere in this library) or float32.
+  // Elements of `dtype`: its own type, or (16 bits, as elsewhere in this library) integers that hold their bits.
   const at::Tensor* elements(const char* name, int dtype) {
     const at::Tensor* t = on_device(name);
-    if (t && (dtype == SDGP_FP32 ? t->scalar_type() != at::kFloat : t->element_size() != 2)) {
+    if (!t) return nullptr;
+    const at::ScalarType type = t->scalar_type();
+    const bool bits = type == at::kShort || type == at::kUInt16;
+    if (dtype == SDGP_FP32   ? type != at::kFloat
+        : dtype == SDGP_FP16 ? type != at::kHalf && !bits
+        : dtype == SDGP_BF16 ? type != at::kBFloat16 && !bits
+                             : t->element_size() != 2) {  // (a dtype that there is not: the call refuses it)
       fail(name, "does not have the elements that dtype names");
+      return nullptr;
+    }
+    return t;
+  }
+  // The compressed pruned copy: values of `dtype` (which the call refuses if they are fp32) and their 16-bit metadata.
+  const at::Tensor* compressed_values(const char* name, int dtype) { return dtype == SDGP_FP32 ? two_bytes(name) : elements(name, dtype); }
+  const at::Tensor* two_bytes(const char* name) {
+    const at::Tensor* t = on_device(name);
+    if (t && t->element_size() != 2) {
+      fail(name, "must hold two bytes an element");
       return nullptr;
     }
     return t;
@@ -401,7 +417,7 @@ ENTRY(token_logprob_backward) {
   const int n = in.i32(), m = in.i32(), scheme = in.i32();
   const uint64_t seed = in.u64();
   in.i32();
-  const at::Tensor *grad = in.elements("grad", dtype), *values = in.elements("values", SDGP_BF16), *meta = in.elements("meta", SDGP_BF16);
+  const at::Tensor *grad = in.elements("grad", dtype), *values = in.compressed_values("values", dtype), *meta = in.two_bytes("meta");
   in.same_numel("grad", grad, rows * K);
   in.same_numel("values", values, rows * (K / 2));
   in.same_numel("meta", meta, rows * (K / 16));
@@ -461,7 +477,7 @@ ENTRY(residual_norm_backward) {
   const int64_t groups = gate && C ? gate->numel() / C : 1;
   const at::Tensor *d_gate = in.of_type("d_gate", at::kFloat, groups * C), *d_post_weight = in.of_type("d_post_weight", at::kFloat, C),
                    *d_pre_weight = in.of_type("d_pre_weight", at::kFloat, C);
-  const at::Tensor *values = in.elements("values", SDGP_BF16), *meta = in.elements("meta", SDGP_BF16), *ws = in.on_device("workspace");
+  const at::Tensor *values = in.compressed_values("values", dtype), *meta = in.two_bytes("meta"), *ws = in.on_device("workspace");
   for (const auto& [name, t] : {std::pair<const char*, const at::Tensor*>{"out", out}, {"d_out", d_out}, {"d_y", d_y}, {"d_residual", d_residual},
                                 {"d_branch", d_branch}})
     in.same_numel(name, t, rows * C);
@@ -479,10 +495,10 @@ ENTRY(residual_norm_backward) {
   });
 }
 
-// A tensor of e4m3 numbers: one byte an element.
-const at::Tensor* bytes_of(LmArgs& in, const char* name) {
+// A tensor of e4m3 numbers, or of bytes that hold their bits.
+const at::Tensor* e4m3(LmArgs& in, const char* name) {
   const at::Tensor* t = given(in, in.on_device(name), name);
-  if (t && t->element_size() != 1) in.fail(name, "must hold one byte an element (float8_e4m3fn or uint8)");
+  if (t && t->scalar_type() != at::kFloat8_e4m3fn && t->scalar_type() != at::kByte) in.fail(name, "must be a float8_e4m3fn or uint8 tensor");
   return t;
 }
 
@@ -491,7 +507,7 @@ ENTRY(fp8_quantize) {  // x, q, scale, block_rows, dtype
   const int dtype = dtype_argument(args, nargs, 5, 4);
   if (PyErr_Occurred()) return nullptr;
   const at::Tensor* x = given(in, in.elements("x", dtype), "x");
-  const at::Tensor* q = bytes_of(in, "q");
+  const at::Tensor* q = e4m3(in, "q");
   const at::Tensor* scale = given(in, in.of_type("scale", at::kFloat, -1), "scale");
   const int block_rows = in.i32();
   in.i32();
@@ -508,9 +524,9 @@ ENTRY(fp8_linear) {  // xq, x_scale, wq, w_scale, y, dtype
   LmArgs in(args, nargs, 6);
   const int dtype = dtype_argument(args, nargs, 6, 5);
   if (PyErr_Occurred()) return nullptr;
-  const at::Tensor* xq = bytes_of(in, "xq");
+  const at::Tensor* xq = e4m3(in, "xq");
   const at::Tensor* x_scale = given(in, in.of_type("x_scale", at::kFloat, -1), "x_scale");
-  const at::Tensor* wq = bytes_of(in, "wq");
+  const at::Tensor* wq = e4m3(in, "wq");
   const at::Tensor* w_scale = given(in, in.of_type("w_scale", at::kFloat, -1), "w_scale");
   const at::Tensor* y = given(in, in.elements("y", dtype), "y");
   in.i32();

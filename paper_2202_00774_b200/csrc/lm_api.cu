@@ -58,7 +58,8 @@ sdgp_status sdgp_token_logprob_backward(const void* logits, const int64_t* targe
 }
 
 static sdgp_status check_norm(int64_t rows, int64_t C, int64_t groups, sdgp_dtype dtype) {
-  if (!valid_dtype(dtype) || rows < 0 || C < 1 || groups < 1 || rows % groups != 0) return SDGP_ERR_INVALID_ARG;
+  if (!valid_dtype(dtype) || rows < 0 || C < 1 || groups < 0) return SDGP_ERR_INVALID_ARG;
+  if (groups == 0 ? rows != 0 : rows % groups != 0) return SDGP_ERR_INVALID_ARG;  // (no rows may have a gate each)
   if (rows > (int64_t)1 << 28 || C > (int64_t)1 << 24) return SDGP_ERR_UNSUPPORTED;
   return SDGP_OK;
 }

@@ -284,7 +284,8 @@ sdgp_status sdgp_fp8_quantize(const void* x, int64_t rows, int64_t K, int block_
  *   y[r, f] = sum_b x_scale[r, b] * w_scale[f / 128, b] * sum_{k in block b} xq[r, k] * wq[f, k]
  * xq [rows, K] with x_scale [rows, ceil(K / 128)], wq [features, K] with w_scale [ceil(features / 128), ceil(K / 128)] (any fp32 numbers),
  * y [rows, features] of element type `dtype`. A block's products are summed on the tensor cores in fp32, blocks are scaled and added in fp32,
- * y is rounded once. The data gradient dO . W is the same call with wq the quantised transpose of W.
+ * y is rounded once. Where the product of a block's two scales leaves fp32's range of normal numbers, its sum is multiplied by one and then by
+ * the other; rows with such a block are computed again by plain multiply-adds, slowly. The data gradient dO . W is the same call with wq the quantised transpose of W.
  * Requirements: K % 16 == 0; xq, wq and y 16-byte aligned; any rows and features. Where rows and features are few, the sum over K is
  * split among multiprocessors; the order of all additions is fixed by the sizes. */
 sdgp_status sdgp_fp8_linear(const void* xq, const float* x_scale, const void* wq, const float* w_scale, void* y, int64_t rows,

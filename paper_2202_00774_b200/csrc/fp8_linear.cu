@@ -4,13 +4,17 @@
 //
 // The scales are any fp32 numbers, so a block's sum has to be multiplied before it is added to the next one's: the tensor cores sum a block
 // of 128 into one of several accumulators in tensor memory, while other warps take an earlier one's sums out, multiply them by the product of
-// the two scales and add them to sums in registers. Two kernels:
+// the two scales and add them to sums in registers. Where that product is no normal number - infinite, subnormal or zero, though the block's
+// share of y need not be -, the sum is multiplied by one scale and then by the other. No ordinary scales are like that, so the rows that have such
+// a block are computed again behind the tensor cores' work, by plain multiply-adds (recompute_rows; 1024 rows of 4096 features, K = 4096: one
+// such row 167 us instead of 20, all of them 10 ms). (Two factors for each sum in the loop itself, behind a test of four blocks' products: 284 us
+// for 16384 rows instead of 258.) Two kernels:
 //
 // Pairs of CTAs (fp8_pair_kernel), for many rows: a pair computes 256 rows of y and 128 features - those of one weight block, so that a row
 // has one scale a block. tcgen05.mma with 256 rows reads both CTAs' halves of the features.
 //   warp 0 TMA producer; warp 1 MMA issuer (first CTA); warps 2, 3 products of scales; warps 4-11 take, scale and store: a thread owns one
 //   row and 64 features, two sums an instruction.
-// What bounds it: 16384 x 4096 . 4096 x 4096 takes 255 us (2.16 PFLOP/s, 64 % of twice the measured burst bf16 rate; 300 us when the chip is
+// What bounds it: 16384 x 4096 . 4096 x 4096 takes 254-262 us (2.1 PFLOP/s, 63 % of twice the measured burst bf16 rate; 300 us when the chip is
 // power-limited, 66 % of twice the sustained one). With the scaling warps doing nothing but hand accumulators back, the same MMAs take 186
 // us; what they add is their instructions on the schedulers that the issuing threads share (single multiply-adds instead of pairs: 273 us).
 //
@@ -18,6 +22,8 @@
 // rows of x, so the weights stream through shared memory once and only T - rows columns are wasted on absent rows of x. The sum over K is
 // split over a cluster of CTAs so that all multiprocessors pull weights; partial sums meet through distributed shared memory in a
 // fixed order. One row, 4096 x 4096: 5.1 us; the weights' bytes alone are 2.6.
+#include <float.h>
+
 #include "dgrad_common.cuh"
 
 namespace sdgp {
@@ -27,6 +33,8 @@ constexpr int kBlockK = 128;            // bytes of a stage's row: one scale blo
 constexpr int kTileBytes = 128 * kBlockK;
 
 struct Fp8Params {
+  const uint8_t *xq, *wq;  // [rows, K], [features, K]
+  int64_t K;
   const float* sx;  // [rows, blocks]
   const float* sw;  // [feature blocks, blocks]
   void* y;          // [rows, features]
@@ -92,6 +100,85 @@ __device__ __forceinline__ void fma_pair(uint64_t& sums, uint32_t x, uint32_t y,
   asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}" : "+l"(sums) : "r"(x), "r"(y), "l"(scale));
 }
 
+// Whether all of some products of scales are normal numbers or NaN, from their least and largest magnitude.
+template <int N>
+__device__ __forceinline__ bool all_normal(const float (&x)[N]) {
+  float least = fabsf(x[0]), most = least;
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    least = fminf(least, fabsf(x[i]));
+    most = fmaxf(most, fabsf(x[i]));
+  }
+  return !(least < FLT_MIN) && !(most > FLT_MAX);
+}
+// What a block's sum v is multiplied by, as (v * first) * second: (1, the scales' product), which leaves v as it is, wherever that product
+// is a normal number or NaN, or a scale is zero. Else the larger scale comes first. Sums of e4m3 products are 0 or from 2^-18 to 2^25: where the
+// scales' product is too large both are above 1 and v * first is no larger than the result; where it is too small, v * first is a normal number
+// if the result is not zero.
+struct Factors {
+  float first, second;
+};
+__device__ __forceinline__ Factors factors_of(float x, float w) {
+  const float product = x * w;
+  if (!(fabsf(product) < FLT_MIN || fabsf(product) > FLT_MAX) || x == 0.0f || w == 0.0f) return {1.0f, product};
+  const bool x_first = fabsf(x) > fabsf(w);
+  return {x_first ? x : w, x_first ? w : x};
+}
+
+// Sixteen products of e4m3 numbers, added up in order.
+__device__ __forceinline__ float add_products(const uint4& a, const uint4& b, float sum) {
+  const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    uint32_t x, w;  // pairs of binary16, exact
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(x) : "h"((uint16_t)(aw[i / 2] >> 16 * (i & 1))));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(w) : "h"((uint16_t)(bw[i / 2] >> 16 * (i & 1))));
+    sum = fmaf(lane_lo<true>(x), lane_lo<true>(w), sum);
+    sum = fmaf(lane_hi<true>(x), lane_hi<true>(w), sum);
+  }
+  return sum;
+}
+
+// Of y's rows [row0, row0 + rows) and `count` features of a block of 128, the rows with a block whose scales want two factors, by `warps` warps
+// of which this is number `warp`.
+__device__ __forceinline__ void recompute_rows(const Fp8Params& p, int64_t row0, int rows, int64_t feature0, int count, int warp, int warps) {
+  const int lane = threadIdx.x & 31;
+  const float* sw = p.sw + feature0 / 128 * p.blocks;
+  for (int r = warp; r < rows; r += warps) {
+    const int64_t row = row0 + r;
+    if (row >= p.rows) break;
+    const float* sx = p.sx + row * p.blocks;
+    bool two = false;
+    for (int b = lane; b < p.blocks; b += 32) two |= factors_of(sx[b], sw[b]).first != 1.0f;
+    if (!__any_sync(0xFFFFFFFFu, two)) continue;
+    for (int i = lane; i < count; i += 32) {
+      const int64_t feature = feature0 + i;
+      if (feature >= p.features) break;
+      const uint8_t *x = p.xq + row * p.K, *w = p.wq + feature * p.K;
+      float sum = 0.0f;
+      for (int b = 0; b < p.blocks; ++b) {
+        float v = 0.0f;
+        const int64_t end = min(p.K, (int64_t)(b + 1) * kBlockK);
+        for (int64_t k = (int64_t)b * kBlockK; k < end; k += 16) v = add_products(*(const uint4*)(x + k), *(const uint4*)(w + k), v);
+        const Factors f = factors_of(sx[b], sw[b]);
+        sum = fmaf(v * f.first, f.second, sum);
+      }
+      const int64_t at = row * p.features + feature;
+      if (p.dtype == SDGP_FP32) ((float*)p.y)[at] = sum;
+      else ((uint16_t*)p.y)[at] = (uint16_t)(p.dtype == SDGP_FP16 ? f32_to_f16_bits(sum) : f32_to_bf16_bits(sum));
+    }
+  }
+}
+
+// The same as a call, where the code inlined made the kernel's loops slower (the kernel of 64 rows 63 instead of 58 us, pairs of CTAs 278 instead of 261).
+__device__ __noinline__ void call_recompute_rows(const Fp8Params p, int64_t row0, int rows, int64_t feature0, int count, int warp, int warps) {
+  recompute_rows(p, row0, rows, feature0, count, warp, warps);
+}
+
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -112,7 +199,7 @@ constexpr int kPairSlack = kSmemSlack + 2 * kScaleFloats * 4 + kStagedBytes;
 
 __global__ void __launch_bounds__(kPairThreads, 1)
 fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmY,
-                const Fp8Params p) {
+                const __grid_constant__ Fp8Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + (-ptx::smem_u32(smem_raw) & 1023u);
   uint8_t* staged = smem + p.stages * kPairStage;
@@ -123,6 +210,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
   uint64_t* scale_full = acc_empty + kPairBufs;
   uint64_t* scale_empty = scale_full + 2;
   uint32_t* tmem_slot = (uint32_t*)(scale_empty + 2);
+  volatile uint32_t* again = tmem_slot + 1;               // some rows are to be computed again
   float* scales = (float*)(staged + kStagedBytes + 256);  // [2][kScaleGroup][128]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
@@ -141,6 +229,7 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       ptx::mbar_init(&scale_full[g], 2);
       ptx::mbar_init(&scale_empty[g], 8);
     }
+    *again = 0u;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&tmX);
     ptx::prefetch_tensormap(&tmW);
@@ -224,10 +313,17 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
           }
           if (!ptx::mbar_wait<kIdleWaitNs>(&scale_empty[g], gph ^ 1u, err, 0x900u + g)) { alive = false; break; }
           float* to = scales + g * kScaleFloats + i;
+          float product[2 * kScaleGroup];
 #pragma unroll
           for (int k = 0; k < kScaleGroup; ++k) {
-            to[k * 128] = x0[k] * w[k];
-            to[k * 128 + 64] = x1[k] * w[k];
+            to[k * 128] = product[2 * k] = x0[k] * w[k];
+            to[k * 128 + 64] = product[2 * k + 1] = x1[k] * w[k];
+          }
+          if (!all_normal(product)) {  // (zero, it may be, because a scale is)
+            bool two = false;
+#pragma unroll
+            for (int k = 0; k < kScaleGroup; ++k) two |= factors_of(x0[k], w[k]).first != 1.0f || factors_of(x1[k], w[k]).first != 1.0f;
+            if (two) *again = 1u;
           }
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(&scale_full[g]);
@@ -315,6 +411,13 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       }
     }
     if (lane == 0) ptx::bulk_wait_group_read<0>();
+    if (*again && alive) {  // (written before the products that the last tile's sums were multiplied by)
+      if (lane == 0) ptx::bulk_wait_group<0>();  // what this warp has stored is in memory
+      __syncwarp();
+      for (int t = first; t < p.tiles; t += pairs)
+        call_recompute_rows(p, (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + (warp & 3) * 32, 32, (int64_t)(t % p.tiles_n) * kPairFeatures + half * kHalf,
+                       kHalf, 0, 1);
+    }
   }
   ptx::tc_fence_before_sync();
   ptx::cluster_sync();
@@ -343,6 +446,7 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
   uint64_t* acc_full = empty + kRowsMaxStages;
   uint64_t* acc_empty = acc_full + kBufs;
   uint32_t* tmem_slot = (uint32_t*)(acc_empty + kBufs);
+  volatile uint32_t* again = tmem_slot + 1;        // some rows are to be computed again
   float* scales = (float*)((uint8_t*)full + 512);  // [2][kRowsGroup][T]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int split = (int)ptx::cluster_nctarank(), rank = (int)ptx::cluster_ctarank();
@@ -357,6 +461,7 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       ptx::mbar_init(&acc_full[a], 1);
       ptx::mbar_init(&acc_empty[a], 4);
     }
+    *again = 0u;
     ptx::fence_mbar_init();
     ptx::prefetch_tensormap(&tmX);
     ptx::prefetch_tensormap(&tmW);
@@ -378,7 +483,7 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
   const int b0 = (int)((int64_t)p.blocks * rank / split), b1 = (int)((int64_t)p.blocks * (rank + 1) / split);
   uint64_t sums[T / 2];  // (of the multiplying warps) pairs of rows of x
   const int f = (warp & 3) * 32 + lane;  // their feature of the block
-  bool alive = true;
+  bool alive = true, normal = true;  // normal: no block wants two factors
 
   if (warp == 0) {
     if (ptx::elect_one()) {
@@ -418,13 +523,15 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
     constexpr int kEach = T * kRowsGroup / 128;
     const int tid = threadIdx.x - 64;
     const float* sw = p.sw + (int64_t)feature_block * p.blocks;
-    float ahead[kEach];
+    float ahead_x[kEach], ahead_w[kEach];  // (1 where there is no row or block)
     auto load = [&](int first) {
 #pragma unroll
       for (int j = 0; j < kEach; ++j) {
         const int64_t row = row0 + (tid + 128 * j) % T;
         const int b = first + (tid + 128 * j) / T;
-        ahead[j] = row < p.rows && b < b1 ? p.sx[row * p.blocks + b] * sw[b] : 0.0f;
+        const bool there = row < p.rows && b < b1;
+        ahead_x[j] = there ? p.sx[row * p.blocks + b] : 1.0f;
+        ahead_w[j] = there ? sw[b] : 1.0f;
       }
     };
 #pragma unroll
@@ -436,8 +543,13 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       const int k = (b - b0) % kRowsGroup, which = ((b - b0) / kRowsGroup) & 1;
       if (k == 0) {
         float* to = scales + which * kRowsGroup * T + tid;
+        float product[kEach];
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) to[128 * j] = ahead[j];
+        for (int j = 0; j < kEach; ++j) to[128 * j] = product[j] = ahead_x[j] * ahead_w[j];
+        if (!all_normal(product)) {  // (zero, it may be, because a scale is)
+#pragma unroll
+          for (int j = 0; j < kEach; ++j) normal &= factors_of(ahead_x[j], ahead_w[j]).first == 1.0f;
+        }
         load(b + kRowsGroup);
         ptx::named_bar_sync(1, 128);  // (who writes the other group's has passed this barrier, so all have read it)
       }
@@ -482,6 +594,7 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       for (int c = 0; c < T; ++c)
         if (c < rows) store(c, acc[c]);
     }
+    if (!normal) *again = 1u;
   } else {
     // partial sums [T][128] over the stages, which every multiplication has read to the end; each CTA adds and stores its share of the rows of
     // x, in the order of the CTAs
@@ -502,11 +615,16 @@ fp8_rows_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
         store(c, sum);
       }
     }
+    if (!normal) st_cluster_u32(ptx::map_to_cta((const void*)again, 0), 1u);
     ptx::cluster_sync();
   }
   ptx::tc_fence_before_sync();
   __syncthreads();
   ptx::tc_fence_after_sync();
+  if (rank == 0 && *again && alive) {
+    if constexpr (T == 64) call_recompute_rows(p, row0, rows, (int64_t)feature_block * 128, 128, warp, kRowsThreads / 32);
+    else recompute_rows(p, row0, rows, (int64_t)feature_block * 128, 128, warp, kRowsThreads / 32);
+  }
   if (warp == 1) ptx::tmem_dealloc(tmem_base, kCols);
 }
 
@@ -576,6 +694,9 @@ cudaError_t take_error_fp8(unsigned int* word) { return take_error_word(word); }
 sdgp_status launch_fp8_linear(const void* xq, const float* x_scale, const void* wq, const float* w_scale, void* y, int64_t rows,
                               int64_t features, int64_t K, int dtype, cudaStream_t stream) {
   Fp8Params p = {};
+  p.xq = (const uint8_t*)xq;
+  p.wq = (const uint8_t*)wq;
+  p.K = K;
   p.sx = x_scale;
   p.sw = w_scale;
   p.y = y;

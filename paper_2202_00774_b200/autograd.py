@@ -247,8 +247,9 @@ def sdgp_linear_logprob(x, weight, targets, classes=None, n=2, m=4, scheme=_b.MA
     """Log probabilities of ``targets`` (int64, the shape of ``x`` without its last dimension; negative: not counted, 0) under the
     logits ``x @ weight.T``, and the entropy of every position: two float32 tensors of the shape of ``targets``. ``weight`` has one
     row for each token; rows past ``classes`` (default: none) are padding to a multiple of 64 and get no probability. The logits'
-    gradient is formed and pruned N:M along the tokens in one pass; ``x``'s gradient is computed from the pruned copy, the weights'
-    from the unpruned one."""
+    gradient is formed and pruned N:M along the tokens (in one pass, where n <= 2 and ``weight`` has a multiple of 128 rows); ``x``'s gradient
+    is computed from the pruned copy, the weights' from the unpruned one. Where ``x`` takes a gradient, in_features and the rows of ``weight``
+    must be multiples of 64 and m 4, 8, 16 or 32: the backward pass refuses others, as ``sdgp_linear``'s does."""
     return _SDGPLinearLogprobFn.apply(x, weight, targets, weight.shape[0] if classes is None else classes, n, m, scheme, seed)
 
 
@@ -312,8 +313,11 @@ def sdgp_linear_residual_norm(x, weight, residual, post_weight=None, pre_weight=
     """The last linear layer of a block with the boundary to the next block:
     ``out = alpha * residual + gate * norm(x @ weight.T) * post_weight`` and ``y = norm(out) * pre_weight`` (root mean square norms;
     without ``post_weight`` the branch is not normalised, without ``pre_weight`` ``y`` is None). ``gate`` has one row, one for each
-    of equal runs of positions (sequences), or one for every position. Returns ``(out, y)``. The layer's dL/dO is formed and pruned
-    N:M along its output features in one pass; gradients of weights and gate are summed in float32."""
+    of equal runs of positions (sequences), or one for every position: its rows are taken in order, whatever its leading dimensions, and not
+    broadcast. ``residual``, the norms' weights and ``gate`` are of the product's element type (bf16 or fp16); others, float32 among them,
+    are refused. Returns ``(out, y)``. The layer's dL/dO is formed and pruned N:M along its output features (in one pass, where n <= 2 and
+    out_features is a multiple of 128); gradients of weights and gate are summed in float32. Where ``x`` takes a gradient, in_features and
+    out_features must be multiples of 64 and m 4, 8, 16 or 32: the backward pass refuses others, as ``sdgp_linear``'s does."""
     return _SDGPLinearResidualNormFn.apply(x, weight, residual, post_weight, pre_weight, gate, alpha, eps, n, m, scheme, seed)
 
 

@@ -308,7 +308,7 @@ struct NormGradParams {
 };
 
 // The pruning function as a call of its own: 24 forms, inlined into none of the kernels that use it (some 100 of their instructions per eight
-// elements, on a path that memory bounds).
+// elements: 16384 x 4096 bf16 with the 2:4 copy take 270 us, 148 without it, 136 by their bytes).
 template <bool F16>
 __device__ __noinline__ uint4 prune_any(uint4 w, int64_t v, uint32_t seed_lo, uint32_t seed_hi, int n, int m, int scheme, int part) {
   uint2 out = make_uint2(0u, 0u);

@@ -249,8 +249,8 @@ sdgp_status sdgp_token_logprob_backward(const void* logits, const int64_t* targe
  *   out = alpha * residual + gate * n              (gate null: 1)
  *   y   = out * rstd(out) * pre_weight             (pre_weight null: no y)
  * branch, residual, out, y [rows, C]; post_weight, pre_weight [C]; gate [groups, C] with rows % groups == 0: row r takes gate
- * r / (rows / groups) (1: the same for all, rows: one each, else one for each sequence). y is formed from the sums in fp32, before `out` is
- * rounded. post_rstd, pre_rstd [rows] f32: what the backward pass wants; each optional. `out` may be `residual` or `branch` itself.
+ * r / (rows / groups) (1: the same for all, rows: one each - none for no rows -, else one for each sequence). y is formed from the sums in
+ * fp32, before `out` is rounded. post_rstd, pre_rstd [rows] f32: what the backward pass wants; each optional. `out` may be `residual` or `branch` itself.
  * Any C up to 2^24, any rows up to 2^28; all tensors of element type `dtype` 16-byte aligned (their rows need not be). */
 sdgp_status sdgp_residual_norm(const void* branch, const void* residual, const void* post_weight, const void* gate, const void* pre_weight,
                                int64_t rows, int64_t C, int64_t groups, float alpha, float eps, sdgp_dtype dtype, void* out, void* y,
@@ -285,7 +285,8 @@ sdgp_status sdgp_fp8_quantize(const void* x, int64_t rows, int64_t K, int block_
  * xq [rows, K] with x_scale [rows, ceil(K / 128)], wq [features, K] with w_scale [ceil(features / 128), ceil(K / 128)] (any fp32 numbers),
  * y [rows, features] of element type `dtype`. A block's products are summed on the tensor cores in fp32, blocks are scaled and added in fp32,
  * y is rounded once. Where the product of a block's two scales leaves fp32's range of normal numbers, its sum is multiplied by one and then by
- * the other; rows with such a block are computed again by plain multiply-adds, slowly. The data gradient dO . W is the same call with wq the quantised transpose of W.
+ * the other; rows with such a block are computed again by plain multiply-adds, slowly. The data gradient dO . W is the same call with wq
+ * the quantised transpose of W.
  * Requirements: K % 16 == 0; xq, wq and y 16-byte aligned; any rows and features. Where rows and features are few, the sum over K is
  * split among multiprocessors; the order of all additions is fixed by the sizes. */
 sdgp_status sdgp_fp8_linear(const void* xq, const float* x_scale, const void* wq, const float* w_scale, void* y, int64_t rows,

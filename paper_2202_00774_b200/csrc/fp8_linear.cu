@@ -415,8 +415,8 @@ fp8_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__
       if (lane == 0) ptx::bulk_wait_group<0>();  // what this warp has stored is in memory
       __syncwarp();
       for (int t = first; t < p.tiles; t += pairs)
-        call_recompute_rows(p, (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + (warp & 3) * 32, 32, (int64_t)(t % p.tiles_n) * kPairFeatures + half * kHalf,
-                       kHalf, 0, 1);
+        call_recompute_rows(p, (int64_t)(t / p.tiles_n) * 256 + (int)rank * 128 + (warp & 3) * 32, 32,
+                            (int64_t)(t % p.tiles_n) * kPairFeatures + half * kHalf, kHalf, 0, 1);
     }
   }
   ptx::tc_fence_before_sync();
